@@ -240,6 +240,139 @@ int stairs_accept_static(const float *logits_dev, int vocab, int ld, int n_req, 
                          const int32_t *draft_dev, int k_max, int32_t *target_tokens_dev,
                          int32_t *accept_len_dev, void *stream);
 
+/* ---------------------------------------------------------------------------------------------
+ * The other steps of a stairs pass on buffers that the caller holds, for programs that run a model
+ * of their own (their projections, their paged cache) and, like the callers of
+ * stairs_accept_static, have no context: block tables and row maps from request lengths, the
+ * append of new keys and values, attention of the new rows over the cache, and acceptance against
+ * sampled tokens.  One pass is
+ *
+ *   stairs_tables_static -> (projections) -> stairs_append_static -> stairs_attend_static
+ *     -> (rest of the model) -> stairs_sample_static or stairs_accept_static
+ *
+ * Common to all of them
+ *  - They allocate no device memory, keep nothing between calls and do not wait.  Work is enqueued
+ *    on `stream` (NULL = default stream) of the current device, on which all buffers must lie; every
+ *    call may be captured into a graph.  Errors: EINVAL, ENOSPC, EUNSUPPORTED, ECUDA, with a text in
+ *    stairs_last_error(NULL); a refused call has enqueued nothing.
+ *  - Lengths and tables are read from the device, so that a pass may follow the one that accepted
+ *    tokens without the host learning how many.  What the host cannot check, the kernels do: an
+ *    index out of its range is skipped as said at each entry, never followed.
+ *  - Rows of a call lie request by request: request i has rows row_off[i] .. row_off[i+1]-1, which
+ *    are its positions n_seq[i], n_seq[i]+1, ...
+ *  - dtype: 0 fp32, 1 bf16, 2 fp16.  Strides are in elements.
+ * --------------------------------------------------------------------------------------------- */
+
+/* A paged K/V cache.  Element (page, token, head, i) of K lies at k_dev + page*page_stride +
+ * token*token_stride + head*head_stride + i, that of V likewise from v_dev: tokens before heads or
+ * heads before tokens, each in any pitch.  Position p of a request is token p % page_tokens of page
+ * block_table[request][p / page_tokens]. */
+typedef struct stairs_paged {
+  void *k_dev, *v_dev;
+  int64_t page_stride, token_stride, head_stride;
+  int32_t n_pages, page_tokens, n_kv_heads, head_dim;
+  int32_t dtype;
+} stairs_paged;
+
+#define STAIRS_TABLES_MAX_REQ 4096
+#define STAIRS_ATTEND_MAX_REQ 4096
+#define STAIRS_MAX_HEAD_DIM 256
+
+/* Block tables and row maps of the next pass, from the requests' lengths.
+ *   n_seq_dev[i], n_new_dev[i]   tokens cached and tokens to come (negative n_new: none)
+ *   n_blocks_in_dev[i]           pages the request holds: entries 0.. of its row of the table
+ *   block_table_dev              (in/out) int32 [n_req, max_blocks]; pages that a request lacks for
+ *                                n_seq + n_new tokens are entered behind those it holds
+ *   free_dev, n_free             int32 list of free pages; entries n_used_in_dev[0].. are handed out
+ *                                in order, first to request 0
+ *   n_blocks_out_dev, n_used_out_dev (out) the two counts after the call; not the same memory as
+ *                                the inputs
+ *   row_off_dev, kv_len_dev      (out) int32 [n_req + 1], [n_req]: first row of each request, and
+ *                                its length with the new tokens
+ *   row_req_dev, row_pos_dev     (out) int32 [max_rows]: request and position of every row
+ *   row_slot_dev                 (out) int64 [max_rows]: page * page_tokens + token of the position,
+ *                                or -1 where the table holds a negative page.  Rows behind the last
+ *                                request's get -1 in all three.
+ *   n_served_dev                 (out) int32 [1].  Requests are served in order: the first one that
+ *                                lacks pages in the list, entries in its row of the table or rows, or
+ *                                whose lengths are no valid ones (negative n_seq, n_blocks outside
+ *                                0..max_blocks), and all behind it get no page and no row.
+ * Limits: 1 <= n_req <= STAIRS_TABLES_MAX_REQ, max_blocks * page_tokens < 2^31. */
+int stairs_tables_static(int n_req, const int32_t *n_seq_dev, const int32_t *n_new_dev,
+                         const int32_t *n_blocks_in_dev, int32_t *block_table_dev, int max_blocks,
+                         int page_tokens, const int32_t *free_dev, int n_free,
+                         const int32_t *n_used_in_dev, int max_rows, int32_t *n_blocks_out_dev,
+                         int32_t *n_used_out_dev, int32_t *row_off_dev, int32_t *kv_len_dev,
+                         int32_t *row_req_dev, int32_t *row_pos_dev, int64_t *row_slot_dev,
+                         int32_t *n_served_dev, void *stream);
+
+/* Files the new rows' keys and values: row t of k_new_dev and v_new_dev (element (t, head, i) at
+ * t*row_stride + head*head_stride + i, type `dtype`) goes to slot row_slot_dev[t] of the cache,
+ * rounded to the cache's type (to nearest, ties to even; beyond its range: infinity).  Rows whose
+ * slot is no slot of the cache (negative, or n_pages * page_tokens and up) are skipped.  A slot named
+ * twice gets one of the two rows, for keys and values each on its own.  n_rows may be 0. */
+int stairs_append_static(const stairs_paged *cache, int n_rows, const void *k_new_dev,
+                         const void *v_new_dev, int dtype, int64_t row_stride, int64_t head_stride,
+                         const int64_t *row_slot_dev, void *stream);
+
+/* Attention of the new rows over the cache.  Row j of request i is position
+ * p = kv_len[i] - (row_off[i+1] - row_off[i]) + j and sees positions 0..p (its own, the cached ones
+ * and the new ones before it: the staircase mask):
+ *   o[t,h] = sum_p' w_p' v[p', h / (n_heads / n_kv_heads)] / sum_p' w_p',
+ *   w_p' = exp(scale * q[t,h].k[p', ...])
+ * A row that sees nothing (p < 0) gets zeros.  Keys and values of positions that a row does not see
+ * have no part in its result, whatever they hold (infinities, NaN), and neither has what lies in the
+ * cache behind a request's last position.  Positions whose table entry is no page of the cache
+ * are not seen by any row.  kv_len is taken as at most max_len, row_off as within 0..n_rows; rows of
+ * no request are left as they were.
+ *   q_dev, o_dev      type of the cache; element (t, head, i) at t*row_stride + head*head_stride + i.
+ *                     o_dev may not overlap the inputs
+ *   max_len           bound of the requests' kv_len; 0: max_blocks * page_tokens
+ *   workspace         stairs_attend_workspace_bytes(), 256-byte aligned: scratch of this call; calls
+ *                     that may overlap on the GPU (and graphs that hold them) need one each
+ * Scores, softmax and sums are 32-bit; of 16-bit caches the softmax weights are rounded to 16 bits for
+ * the product with V.  Limits: 1 <= n_req <= STAIRS_ATTEND_MAX_REQ, head_dim <= STAIRS_MAX_HEAD_DIM,
+ * n_heads a multiple of n_kv_heads. */
+size_t stairs_attend_workspace_bytes(const stairs_paged *cache, int n_heads, int n_req, int n_rows);
+int stairs_attend_static(const stairs_paged *cache, const int32_t *block_table_dev, int max_blocks,
+                         int n_req, const int32_t *row_off_dev, const int32_t *kv_len_dev, int max_len,
+                         int n_rows, int n_heads, const void *q_dev, int64_t q_row_stride,
+                         int64_t q_head_stride, float scale, void *o_dev, int64_t o_row_stride,
+                         int64_t o_head_stride, void *workspace, size_t workspace_bytes, void *stream);
+
+/* How the tokens of one request's rows are drawn. */
+typedef struct stairs_sampling {
+  float temperature; /* 0: the greedy token; else 1e-6 .. 1e6                            */
+  int32_t top_k;     /* 0: no limit                                                      */
+  float top_p;       /* in (0, 1]; 1: no limit                                           */
+  float min_p;       /* in [0, 1]; 0: no limit                                           */
+} stairs_sampling;
+
+/* Sampled acceptance: stairs_accept_static with a token drawn for every row in place of the greedy
+ * one.  Of row t with scores x and the random number u_dev[t] in [0, 1):
+ *   w_i = exp((x_i - max x) / temperature)
+ *   kept are the tokens with w_i >= min_p; of these the top_k of largest x (the lower index first
+ *   among equal ones); of these, in that order, the first whose weights sum up to at least top_p of
+ *   what they all weigh
+ *   the token is the lowest index at which the running sum of the kept weights, in the order of the
+ *   indices, exceeds u times their sum
+ * Temperature 0: the greedy token, lowest index on ties.  Scores of -infinity and NaN are never drawn; a
+ * row that has no other gets -1.  Where x holds +infinity, only such tokens weigh (1 each).
+ * A drafted token is kept while it equals the token drawn for the row before it, so the
+ * tokens kept and the one after them are distributed as the model's own, drawn one by one.
+ * Weights are held to 2^-47 of the largest and summed exactly, so a row's token depends neither on
+ * the rest of the call nor on the device's timing.
+ *   logits_dev          [n_rows, ld] of `dtype`, rows request by request
+ *   params_host         [n_req]
+ *   draft_dev, k_max, target_tokens_dev, accept_len_dev   as for stairs_accept_static
+ * Limits: 1 <= n_req <= STAIRS_SAMPLE_MAX_REQ, n_rows <= STAIRS_STATIC_MAX_ROWS, k_max <= 63,
+ * vocab <= 2^20. */
+#define STAIRS_SAMPLE_MAX_REQ 256
+int stairs_sample_static(const void *logits_dev, int dtype, int vocab, int64_t ld, int n_req,
+                         const int32_t *k_host, const stairs_sampling *params_host, const float *u_dev,
+                         const int32_t *draft_dev, int k_max, int32_t *target_tokens_dev,
+                         int32_t *accept_len_dev, void *stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -41,7 +41,7 @@ def build(force: bool = False, verbose: bool = False) -> str:
     """Compiles csrc/*.cu into libstairs_b200.so (skipped when up to date).  Returns the path."""
     if not force and not _stale():
         return LIB_PATH
-    jobs = [("engine.cu", [])] + [("forward.cu", ["-DFWD_HD=%d" % hd, "-DFWD_FAM=%d" % fam, "-DFWD_ATT=%d" % att, "-DFWD_ONE=%d" % one, "-DFWD_SHARE=%d" % share])
+    jobs = [("engine.cu", []), ("attend.cu", []), ("sample.cu", []), ("paged.cu", [])] + [("forward.cu", ["-DFWD_HD=%d" % hd, "-DFWD_FAM=%d" % fam, "-DFWD_ATT=%d" % att, "-DFWD_ONE=%d" % one, "-DFWD_SHARE=%d" % share])
                                   for hd, fam, att, one, share in FORWARD]
     log = ""
     failed = False

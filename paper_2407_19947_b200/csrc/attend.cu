@@ -1,0 +1,140 @@
+// Attention of new rows over a caller's paged cache (stairs_attend_static).
+//
+//   o[t,h] = sum_p w_p v[p] / sum_p w_p,   w_p = exp(scale q[t,h].k[p] - m),   m = max over the seen positions
+//
+// with the running maximum and sum of a softmax, so that K and V are read once.
+#include <algorithm>
+#include <type_traits>
+
+#include "static_ops.cuh"
+
+namespace stairs {
+namespace {
+
+struct AttendParams {
+  const void* kc; const void* vc; const void* q; void* o;
+  long long page_stride, token_stride, head_stride, q_row, q_head, o_row, o_head;
+  const int* table; const int* row_off; const int* kv_len;
+  int n_req, n_rows, heads, kv_heads, hd, n_pages, page_tokens, max_blocks, max_len;
+  float scale;
+  float* part;                  // partial states of split units
+};
+
+__device__ __forceinline__ int clampi(int v, int lo, int hi) { return v < lo ? lo : (v > hi ? hi : v); }
+
+// ------------------------------------------------------------------------------------------------
+// Any type, stride, alignment and head size: one block per row and head, one warp per 32 positions in turn.  Every element is
+// loaded by itself, so this is the form of last resort: caches whose vectors do not start on 16 bytes.
+// ------------------------------------------------------------------------------------------------
+constexpr int AP_WARPS = 4;
+template <typename T> __global__ void __launch_bounds__(AP_WARPS * 32) k_attend_plain(const AttendParams P) {
+  __shared__ float qs[STAIRS_MAX_HEAD_DIM], accs[AP_WARPS][STAIRS_MAX_HEAD_DIM], ms[AP_WARPS], ls[AP_WARPS];
+  wait_prerequisites();
+  const int h = blockIdx.x % P.heads, t = blockIdx.x / P.heads, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  int lo = 0, hi = P.n_req - 1;              // the last request whose first row is <= t
+  while (lo < hi) {
+    const int mid = (lo + hi + 1) >> 1;
+    if (P.row_off[mid] <= t) lo = mid; else hi = mid - 1;
+  }
+  const int first = max(P.row_off[lo], 0), end = min(P.row_off[lo + 1], P.n_rows);
+  if (t < first || t >= end) return;         // a row of no request
+  const int last = clampi(P.kv_len[lo], 0, P.max_len) - (end - first) + (t - first);
+  const int* table = P.table + (size_t)lo * P.max_blocks;
+  const T* q = reinterpret_cast<const T*>(P.q) + t * P.q_row + h * P.q_head;
+  const T* kc = reinterpret_cast<const T*>(P.kc) + (h / (P.heads / P.kv_heads)) * P.head_stride;
+  const T* vc = reinterpret_cast<const T*>(P.vc) + (h / (P.heads / P.kv_heads)) * P.head_stride;
+  for (int i = threadIdx.x; i < P.hd; i += AP_WARPS * 32) qs[i] = to_f32(q[i]) * P.scale;
+  __syncthreads();
+  constexpr int ND = STAIRS_MAX_HEAD_DIM / 32;
+  float m = -INFINITY, l = 0.f, acc[ND];
+#pragma unroll
+  for (int i = 0; i < ND; ++i) acc[i] = 0.f;
+  for (int base = warp * 32; base <= last; base += AP_WARPS * 32) {
+    const int p = base + lane;
+    long long at = -1;
+    float s = -INFINITY;
+    if (p <= last) {
+      const int page = table[p / P.page_tokens];
+      if (page >= 0 && page < P.n_pages) {
+        at = page * P.page_stride + (p % P.page_tokens) * P.token_stride;
+        float dot = 0.f;
+        for (int d = 0; d < P.hd; ++d) dot = fmaf(qs[d], to_f32(kc[at + d]), dot);
+        s = dot;
+      }
+    }
+    const float m_new = fmaxf(m, warp_max(s));
+    const float ref = m_new == -INFINITY ? 0.f : m_new;
+    const float w = expf(s - ref), corr = expf(m - ref);
+    l = l * corr + warp_sum(w);
+    m = m_new;
+#pragma unroll
+    for (int i = 0; i < ND; ++i) acc[i] *= corr;
+    for (int j = 0; j < 32; ++j) {
+      const float wj = __shfl_sync(0xffffffffu, w, j);
+      const long long aj = __shfl_sync(0xffffffffu, at, j);
+      if (aj < 0) continue;
+#pragma unroll
+      for (int i = 0; i < ND; ++i) {
+        const int d = lane + 32 * i;
+        if (d < P.hd) acc[i] = fmaf(wj, to_f32(vc[aj + d]), acc[i]);
+      }
+    }
+  }
+  if (lane == 0) { ms[warp] = m; ls[warp] = l; }
+#pragma unroll
+  for (int i = 0; i < ND; ++i) if (lane + 32 * i < P.hd) accs[warp][lane + 32 * i] = acc[i];
+  __syncthreads();
+  float M = -INFINITY, L = 0.f, f[AP_WARPS];
+#pragma unroll
+  for (int w = 0; w < AP_WARPS; ++w) M = fmaxf(M, ms[w]);
+#pragma unroll
+  for (int w = 0; w < AP_WARPS; ++w) { f[w] = ms[w] == -INFINITY ? 0.f : expf(ms[w] - M); L += ls[w] * f[w]; }
+  const float inv = M == -INFINITY ? 0.f : 1.0f / L;
+  T* o = reinterpret_cast<T*>(P.o) + t * P.o_row + h * P.o_head;
+  for (int d = threadIdx.x; d < P.hd; d += AP_WARPS * 32) {
+    float v = 0.f;
+#pragma unroll
+    for (int w = 0; w < AP_WARPS; ++w) if (f[w] != 0.f) v += accs[w][d] * f[w];
+    o[d] = from_f32<T>(v * inv);
+  }
+}
+
+}  // namespace
+}  // namespace stairs
+
+using namespace stairs;
+
+extern "C" size_t stairs_attend_workspace_bytes(const stairs_paged* cache, int n_heads, int n_req, int n_rows) {
+  if (check_paged("stairs_attend_workspace_bytes", cache)) return 0;
+  return 256;
+}
+
+extern "C" int stairs_attend_static(const stairs_paged* cache, const int32_t* block_table_dev, int max_blocks, int n_req, const int32_t* row_off_dev,
+                                    const int32_t* kv_len_dev, int max_len, int n_rows, int n_heads, const void* q_dev, int64_t q_row_stride,
+                                    int64_t q_head_stride, float scale, void* o_dev, int64_t o_row_stride, int64_t o_head_stride, void* workspace,
+                                    size_t workspace_bytes, void* stream) {
+  const char* who = "stairs_attend_static";
+  if (int rc = check_paged(who, cache)) return rc;
+  if (!block_table_dev || !row_off_dev || !kv_len_dev) return static_fail(STAIRS_EINVAL, "%s: NULL buffer", who);
+  if (n_req < 1 || n_req > STAIRS_ATTEND_MAX_REQ) return static_fail(STAIRS_ENOSPC, "%s: n_req=%d outside 1..%d", who, n_req, STAIRS_ATTEND_MAX_REQ);
+  if (max_blocks < 1 || (long long)max_blocks * cache->page_tokens >= (1ll << 31))
+    return static_fail(STAIRS_EINVAL, "%s: max_blocks=%d of %d tokens", who, max_blocks, cache->page_tokens);
+  if (max_len < 0 || n_rows < 0 || q_row_stride < 0 || q_head_stride < 0 || o_row_stride < 0 || o_head_stride < 0)
+    return static_fail(STAIRS_EINVAL, "%s: max_len=%d, n_rows=%d or a stride is negative", who, max_len, n_rows);
+  if (n_heads < 1 || n_heads % cache->n_kv_heads) return static_fail(STAIRS_EINVAL, "%s: %d heads for %d key heads", who, n_heads, cache->n_kv_heads);
+  if (!(fabsf(scale) < INFINITY)) return static_fail(STAIRS_EINVAL, "%s: scale is not finite", who);
+  if (n_rows == 0) return STAIRS_OK;
+  if (!q_dev || !o_dev) return static_fail(STAIRS_EINVAL, "%s: NULL buffer", who);
+  if ((long long)n_rows * n_heads > 0x7fffffffll) return static_fail(STAIRS_ENOSPC, "%s: %d rows of %d heads are too many", who, n_rows, n_heads);
+  const int reach = max_blocks * cache->page_tokens;
+  AttendParams P{cache->k_dev, cache->v_dev, q_dev, o_dev, cache->page_stride, cache->token_stride, cache->head_stride, q_row_stride, q_head_stride,
+                 o_row_stride, o_head_stride, block_table_dev, row_off_dev, kv_len_dev, n_req, n_rows, n_heads, cache->n_kv_heads, cache->head_dim,
+                 cache->n_pages, cache->page_tokens, max_blocks, max_len ? std::min(max_len, reach) : reach, scale, nullptr};
+  cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
+  const unsigned blocks = (unsigned)(n_rows * n_heads);
+  if (cache->dtype == DT_F32) k_attend_plain<float><<<blocks, AP_WARPS * 32, 0, st>>>(P);
+  else if (cache->dtype == DT_BF16) k_attend_plain<bf16><<<blocks, AP_WARPS * 32, 0, st>>>(P);
+  else k_attend_plain<__half><<<blocks, AP_WARPS * 32, 0, st>>>(P);
+  SCK(cudaGetLastError());
+  return STAIRS_OK;
+}

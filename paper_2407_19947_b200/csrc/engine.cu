@@ -21,6 +21,7 @@
 #include "megakernel.cuh"
 #include "mid.cuh"
 #include "small_f32.cuh"
+#include "static_ops.cuh"
 #include "wide.cuh"
 
 using namespace stairs;
@@ -136,6 +137,21 @@ int fail(stairs_ctx* c, int code, const char* fmt, ...) {
   if (c) c->err = buf; else g_init_error = buf;
   return code;
 }
+
+}  // namespace
+
+// the same for the entry points without a context that live in other files (see static_ops.cuh)
+int stairs::static_fail(int code, const char* fmt, ...) {
+  char buf[512];
+  va_list ap;
+  va_start(ap, fmt);
+  vsnprintf(buf, sizeof buf, fmt, ap);
+  va_end(ap);
+  try { g_init_error = buf; } catch (...) {}   // (the text is lost where there is no memory for it)
+  return code;
+}
+
+namespace {
 
 #define CK(call)                                                                              \
   do {                                                                                        \

@@ -1,0 +1,234 @@
+// Block tables and row maps from request lengths (stairs_tables_static) and the append of new keys and
+// values to a paged cache (stairs_append_static).
+#include <algorithm>
+#include <type_traits>
+
+#include "static_ops.cuh"
+
+namespace stairs {
+
+int check_paged(const char* who, const stairs_paged* c) {
+  if (!c || !c->k_dev || !c->v_dev) return static_fail(STAIRS_EINVAL, "%s: NULL cache", who);
+  if (c->dtype < DT_F32 || c->dtype > DT_F16) return static_fail(STAIRS_EINVAL, "%s: cache dtype %d", who, c->dtype);
+  if (c->n_pages < 1 || c->page_tokens < 1 || c->n_kv_heads < 1 || c->head_dim < 1)
+    return static_fail(STAIRS_EINVAL, "%s: cache of %d pages, %d tokens a page, %d heads of %d", who, c->n_pages, c->page_tokens, c->n_kv_heads, c->head_dim);
+  if (c->head_dim > STAIRS_MAX_HEAD_DIM) return static_fail(STAIRS_EUNSUPPORTED, "%s: head_dim %d above %d", who, c->head_dim, STAIRS_MAX_HEAD_DIM);
+  if (c->page_stride < 0 || c->token_stride < 0 || c->head_stride < 0) return static_fail(STAIRS_EINVAL, "%s: negative stride", who);
+  return STAIRS_OK;
+}
+
+namespace {
+
+// ------------------------------------------------------------------------------------------------
+// Tables
+// ------------------------------------------------------------------------------------------------
+struct TablesParams {
+  int n_req, max_blocks, page_tokens, n_free, max_rows;
+  const int* n_seq; const int* n_new; const int* n_blocks_in; const int* free_list; const int* n_used_in;
+  int* table; int* n_blocks_out; int* n_used_out; int* row_off; int* kv_len; int* row_req; int* row_pos; long long* row_slot; int* n_served;
+};
+
+constexpr int TB_THREADS = 512, TB_ROWS = 2048;   // rows per block
+
+__device__ __forceinline__ long long warp_scan(long long v, int lane) {
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const long long u = __shfl_up_sync(0xffffffffu, v, o);
+    if (lane >= o) v += u;
+  }
+  return v;
+}
+
+// Requests are served in order, so what each gets is two running sums: of the pages lacking and of the rows.  Every block computes them
+// for all requests (the lengths are a few KB from L2) and then files a part of the rows and of the requests' new pages; a row's slot
+// takes a page that this call hands out from the free list itself, never from the table, which another block writes.  A call is
+// bound by latency: one launch, two dependent loads, a scan, a search in shared memory.
+__global__ void __launch_bounds__(TB_THREADS) k_tables(const TablesParams P) {
+  extern __shared__ int tb_sm[];
+  int* s_off = tb_sm;                       // [n_req + 1] first row
+  int* s_first = s_off + P.n_req + 1;       // [n_req] place of the first new page in the free list
+  int* s_seq = s_first + P.n_req;           // [n_req]
+  int* s_had = s_seq + P.n_req;             // [n_req]
+  __shared__ long long w_pages[TB_THREADS / 32], w_rows[TB_THREADS / 32];
+  __shared__ int s_served;
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  wait_prerequisites();
+  const int used0 = P.n_used_in[0];
+  if (tid == 0) { s_served = P.n_req; s_off[0] = 0; }
+  long long pages_before = 0, rows_before = 0;
+  bool stopped = used0 < 0;                  // (a count that is none: nothing is handed out)
+  for (int base = 0; base < P.n_req; base += TB_THREADS) {
+    const int i = base + tid;
+    const bool on = i < P.n_req;
+    const int seq = on ? P.n_seq[i] : 0, new_i = on ? max(P.n_new[i], 0) : 0, had = on ? P.n_blocks_in[i] : 0;
+    const long long want = ((long long)seq + new_i + P.page_tokens - 1) / P.page_tokens;
+    const long long need = max(want - had, 0ll);
+    const bool valid = seq >= 0 && had >= 0 && had <= P.max_blocks && had + need <= P.max_blocks;
+    long long pages = valid ? need : 0, rows = valid ? new_i : 0;
+    const long long sp = warp_scan(pages, lane), sr = warp_scan(rows, lane);
+    if (lane == 31) { w_pages[warp] = sp; w_rows[warp] = sr; }
+    __syncthreads();
+    if (warp == 0) {
+      const long long a = warp_scan(lane < TB_THREADS / 32 ? w_pages[lane] : 0, lane), b = warp_scan(lane < TB_THREADS / 32 ? w_rows[lane] : 0, lane);
+      if (lane < TB_THREADS / 32) { w_pages[lane] = a; w_rows[lane] = b; }
+    }
+    __syncthreads();
+    const long long end_p = pages_before + (warp ? w_pages[warp - 1] : 0) + sp, end_r = rows_before + (warp ? w_rows[warp - 1] : 0) + sr;
+    const bool fits = valid && !stopped && (long long)used0 + end_p <= P.n_free && end_r <= P.max_rows;
+    if (on && !fits) atomicMin(&s_served, i);
+    if (on) { s_off[i + 1] = (int)min(end_r, (long long)P.max_rows); s_first[i] = (int)min(used0 + end_p - pages, (long long)P.n_free); s_seq[i] = seq; s_had[i] = had; }
+    pages_before += w_pages[TB_THREADS / 32 - 1]; rows_before += w_rows[TB_THREADS / 32 - 1];
+    __syncthreads();
+  }
+  const int served = s_served;
+  const int total = s_off[served];
+  // requests: this block's share
+  const int per_req = (P.n_req + gridDim.x - 1) / gridDim.x, r0 = blockIdx.x * per_req, r1 = min(P.n_req, r0 + per_req);
+  for (int i = r0 + tid; i < r1; i += TB_THREADS) {
+    const bool on = i < served;
+    const int rows = on ? s_off[i + 1] - s_off[i] : 0;
+    P.row_off[i] = on ? s_off[i] : total;
+    P.kv_len[i] = s_seq[i] + rows;
+    const int need = on ? max((int)(((long long)s_seq[i] + rows + P.page_tokens - 1) / P.page_tokens) - s_had[i], 0) : 0;
+    P.n_blocks_out[i] = s_had[i] + need;
+    if (i == served - 1) { P.n_used_out[0] = s_first[i] + need; }
+  }
+  if (blockIdx.x == 0 && tid == 0) {
+    if (served == 0) P.n_used_out[0] = used0;
+    P.row_off[P.n_req] = total;
+    P.n_served[0] = served;
+  }
+  // new table entries: one warp per request
+  for (int i = r0 + warp; i < min(r1, served); i += TB_THREADS / 32) {
+    const int rows = s_off[i + 1] - s_off[i], had = s_had[i];
+    const int need = max((int)(((long long)s_seq[i] + rows + P.page_tokens - 1) / P.page_tokens) - had, 0);
+    for (int b = lane; b < need; b += 32) P.table[(size_t)i * P.max_blocks + had + b] = P.free_list[s_first[i] + b];
+  }
+  // rows
+  const int t1 = min(P.max_rows, (int)(blockIdx.x + 1) * TB_ROWS);
+  for (int t = blockIdx.x * TB_ROWS + tid; t < t1; t += TB_THREADS) {
+    int req = -1, pos = -1;
+    long long slot = -1;
+    if (t < total) {
+      int lo = 0, hi = served - 1;           // the last request whose first row is <= t (requests without rows are passed over)
+      while (lo < hi) {
+        const int mid = (lo + hi + 1) >> 1;
+        if (s_off[mid] <= t) lo = mid; else hi = mid - 1;
+      }
+      req = lo;
+      pos = s_seq[req] + t - s_off[req];
+      const int block = pos / P.page_tokens, fresh = block - s_had[req];
+      const int page = fresh >= 0 ? P.free_list[s_first[req] + fresh] : P.table[(size_t)req * P.max_blocks + block];
+      if (page >= 0) slot = (long long)page * P.page_tokens + (pos - block * P.page_tokens);
+    }
+    P.row_req[t] = req; P.row_pos[t] = pos; P.row_slot[t] = slot;
+  }
+}
+
+// ------------------------------------------------------------------------------------------------
+// Append
+// ------------------------------------------------------------------------------------------------
+struct AppendParams {
+  const void* k; const void* v; void* kc; void* vc;
+  const long long* slot;
+  long long row_stride, head_stride, page_stride, token_stride, cache_head_stride, n_slots;
+  int n_rows, heads, head_dim, page_tokens;
+};
+
+// One thread: VEC elements of a row's keys or values (blockIdx.z), from and to consecutive addresses.  Bound by the bytes, read and written once;
+// small calls by latency.  VEC elements are 16 bytes of the wider of the two types (VEC 1: any address).
+template <typename S, typename D, int VEC>
+__global__ void __launch_bounds__(256) k_append(const AppendParams P) {
+  wait_prerequisites();
+  const int pieces = P.head_dim / VEC, per_row = P.heads * pieces;
+  const long long it = (long long)blockIdx.x * 256 + threadIdx.x;
+  if (it >= (long long)P.n_rows * per_row) return;
+  const int t = (int)(it / per_row), in_row = (int)(it - (long long)t * per_row), h = in_row / pieces, i = (in_row - h * pieces) * VEC;
+  const long long slot = P.slot[t];
+  if (slot < 0 || slot >= P.n_slots) return;
+  const long long page = slot / P.page_tokens, token = slot - page * P.page_tokens;
+  const S* src = reinterpret_cast<const S*>(blockIdx.z ? P.v : P.k) + t * P.row_stride + h * P.head_stride + i;
+  D* dst = reinterpret_cast<D*>(blockIdx.z ? P.vc : P.kc) + page * P.page_stride + token * P.token_stride + h * P.cache_head_stride + i;
+  struct alignas(VEC * sizeof(S)) VS { S e[VEC]; };
+  struct alignas(VEC * sizeof(D)) VD { D e[VEC]; };
+  const VS x = *reinterpret_cast<const VS*>(src);
+  VD y;
+#pragma unroll
+  for (int j = 0; j < VEC; ++j) {
+    if constexpr (sizeof(S) == sizeof(D) && std::is_same<S, D>::value) y.e[j] = x.e[j];   // (bit for bit)
+    else y.e[j] = from_f32<D>(to_f32(x.e[j]));
+  }
+  *reinterpret_cast<VD*>(dst) = y;
+}
+
+template <typename S, typename D> int launch_append(const AppendParams& P, bool vec, cudaStream_t st) {
+  constexpr int V = 16 / (sizeof(S) > sizeof(D) ? sizeof(S) : sizeof(D));
+  const long long threads = (long long)P.n_rows * P.heads * (P.head_dim / (vec ? V : 1));
+  const long long blocks = (threads + 255) / 256;
+  if (blocks > 0x7fffffffll) return static_fail(STAIRS_ENOSPC, "stairs_append_static: %d rows are too many", P.n_rows);
+  if (vec) k_append<S, D, V><<<dim3((unsigned)blocks, 1, 2), 256, 0, st>>>(P);
+  else k_append<S, D, 1><<<dim3((unsigned)blocks, 1, 2), 256, 0, st>>>(P);
+  SCK(cudaGetLastError());
+  return STAIRS_OK;
+}
+
+}  // namespace
+}  // namespace stairs
+
+using namespace stairs;
+
+extern "C" int stairs_tables_static(int n_req, const int32_t* n_seq_dev, const int32_t* n_new_dev, const int32_t* n_blocks_in_dev,
+                                    int32_t* block_table_dev, int max_blocks, int page_tokens, const int32_t* free_dev, int n_free,
+                                    const int32_t* n_used_in_dev, int max_rows, int32_t* n_blocks_out_dev, int32_t* n_used_out_dev,
+                                    int32_t* row_off_dev, int32_t* kv_len_dev, int32_t* row_req_dev, int32_t* row_pos_dev,
+                                    int64_t* row_slot_dev, int32_t* n_served_dev, void* stream) {
+  const char* who = "stairs_tables_static";
+  if (!n_seq_dev || !n_new_dev || !n_blocks_in_dev || !block_table_dev || !n_used_in_dev || !n_blocks_out_dev || !n_used_out_dev || !row_off_dev ||
+      !kv_len_dev || !n_served_dev || (n_free > 0 && !free_dev) || (max_rows > 0 && (!row_req_dev || !row_pos_dev || !row_slot_dev)))
+    return static_fail(STAIRS_EINVAL, "%s: NULL buffer", who);
+  if (n_req < 1 || n_req > STAIRS_TABLES_MAX_REQ) return static_fail(STAIRS_ENOSPC, "%s: n_req=%d outside 1..%d", who, n_req, STAIRS_TABLES_MAX_REQ);
+  if (max_blocks < 1 || page_tokens < 1 || n_free < 0 || max_rows < 0)
+    return static_fail(STAIRS_EINVAL, "%s: max_blocks=%d, page_tokens=%d, n_free=%d, max_rows=%d", who, max_blocks, page_tokens, n_free, max_rows);
+  if ((long long)max_blocks * page_tokens >= (1ll << 31)) return static_fail(STAIRS_EINVAL, "%s: max_blocks * page_tokens beyond 31 bits", who);
+  if (max_rows > 0x7fffffff - TB_ROWS) return static_fail(STAIRS_EINVAL, "%s: max_rows=%d", who, max_rows);
+  if (n_blocks_out_dev == n_blocks_in_dev || n_used_out_dev == n_used_in_dev) return static_fail(STAIRS_EINVAL, "%s: a count's output is its input", who);
+  TablesParams P{n_req, max_blocks, page_tokens, n_free, max_rows, n_seq_dev, n_new_dev, n_blocks_in_dev, free_dev, n_used_in_dev,
+                 block_table_dev, n_blocks_out_dev, n_used_out_dev, row_off_dev, kv_len_dev, row_req_dev, row_pos_dev,
+                 reinterpret_cast<long long*>(row_slot_dev), n_served_dev};
+  const int smem = (4 * n_req + 1) * 4;
+  if (smem > 48 * 1024) SCK(cudaFuncSetAttribute(k_tables, cudaFuncAttributeMaxDynamicSharedMemorySize, (4 * STAIRS_TABLES_MAX_REQ + 1) * 4));
+  const int blocks = std::max(1, (max_rows + TB_ROWS - 1) / TB_ROWS);
+  k_tables<<<blocks, TB_THREADS, smem, reinterpret_cast<cudaStream_t>(stream)>>>(P);
+  SCK(cudaGetLastError());
+  return STAIRS_OK;
+}
+
+extern "C" int stairs_append_static(const stairs_paged* cache, int n_rows, const void* k_new_dev, const void* v_new_dev, int dtype,
+                                    int64_t row_stride, int64_t head_stride, const int64_t* row_slot_dev, void* stream) {
+  const char* who = "stairs_append_static";
+  if (int rc = check_paged(who, cache)) return rc;
+  if (n_rows < 0 || row_stride < 0 || head_stride < 0) return static_fail(STAIRS_EINVAL, "%s: n_rows=%d or a stride is negative", who, n_rows);
+  if (dtype < DT_F32 || dtype > DT_F16) return static_fail(STAIRS_EINVAL, "%s: dtype %d", who, dtype);
+  if (n_rows == 0) return STAIRS_OK;
+  if (!k_new_dev || !v_new_dev || !row_slot_dev) return static_fail(STAIRS_EINVAL, "%s: NULL buffer", who);
+  AppendParams P{k_new_dev, v_new_dev, cache->k_dev, cache->v_dev, reinterpret_cast<const long long*>(row_slot_dev), row_stride, head_stride,
+                 cache->page_stride, cache->token_stride, cache->head_stride, (long long)cache->n_pages * cache->page_tokens,
+                 n_rows, cache->n_kv_heads, cache->head_dim, cache->page_tokens};
+  // whole vectors where every element group of the vector starts on its own boundary in both places
+  const int es = dtype_bytes(dtype), ed = dtype_bytes(cache->dtype), V = 16 / std::max(es, ed);
+  auto on = [&](const void* p, int e) { return reinterpret_cast<uintptr_t>(p) % (size_t)(V * e) == 0; };
+  const bool vec = cache->head_dim % V == 0 && row_stride % V == 0 && head_stride % V == 0 && cache->page_stride % V == 0 && cache->token_stride % V == 0 &&
+                   cache->head_stride % V == 0 && on(k_new_dev, es) && on(v_new_dev, es) && on(cache->k_dev, ed) && on(cache->v_dev, ed);
+  cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
+  switch (dtype * 3 + cache->dtype) {
+    case 0: return launch_append<float, float>(P, vec, st);
+    case 1: return launch_append<float, bf16>(P, vec, st);
+    case 2: return launch_append<float, __half>(P, vec, st);
+    case 3: return launch_append<bf16, float>(P, vec, st);
+    case 4: return launch_append<bf16, bf16>(P, vec, st);
+    case 5: return launch_append<bf16, __half>(P, vec, st);
+    case 6: return launch_append<__half, float>(P, vec, st);
+    case 7: return launch_append<__half, bf16>(P, vec, st);
+    default: return launch_append<__half, __half>(P, vec, st);
+  }
+}

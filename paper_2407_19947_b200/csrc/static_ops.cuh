@@ -1,0 +1,33 @@
+// What the entry points on caller-held buffers (paged.cu, attend.cu, sample.cu) share.
+#pragma once
+#include "../../include/stairs.h"
+#include "common.cuh"
+
+namespace stairs {
+
+// Files the text that stairs_last_error(NULL) gives and returns `code`.
+int static_fail(int code, const char* fmt, ...);
+
+#define SCK(call)                                                                                       \
+  do {                                                                                                  \
+    cudaError_t e_ = (call);                                                                            \
+    if (e_ != cudaSuccess)                                                                              \
+      return stairs::static_fail(STAIRS_ECUDA, "%s failed: %s (%s:%d)", #call, cudaGetErrorString(e_),  \
+                                 __FILE__, __LINE__);                                                   \
+  } while (0)
+
+enum Dtype { DT_F32 = 0, DT_BF16 = 1, DT_F16 = 2 };
+inline int dtype_bytes(int dt) { return dt == DT_F32 ? 4 : 2; }
+
+inline bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
+
+// Checks that every entry point with a cache makes; 0 or a status with its text filed.
+int check_paged(const char* who, const stairs_paged* c);
+
+// PDL: the next kernel of the stream may be set up; wait until the previous one's writes are visible.
+__device__ __forceinline__ void launch_dependents() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
+__device__ __forceinline__ void wait_prerequisites() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+
+__device__ __forceinline__ uint32_t smem_addr(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
+
+}  // namespace stairs
