@@ -17,6 +17,7 @@ LIB_PATH = os.path.join(HERE, "libstairs_b200.so")
 # variants of the whole-pass kernel (head size, model family, attention path, at most 16 rows, shared rows), one object each
 FORWARD = [v + (s,) for s in (0, 1) for v in ([(64, 1, a, o) for a in (0, 1) for o in (0, 1)] + [(64, 2, a, o) for a in (0, 1) for o in (0, 1)] +
            [(80, 2, 0, o) for o in (0, 1)] + [(128, 2, a, o) for a in (0, 1) for o in (0, 1)] + [(0, 0, 3, 0)])]
+ATTEND_STEPS = (2, 4, 5, 6, 8, 12, 16)   # head sizes of the split attention kernel, in steps of 16
 NVCC_FLAGS = ["-O3", "-std=c++17", "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo",
               "-Xcompiler", "-fPIC", "--expt-relaxed-constexpr", "-Xptxas", "-v"]
 
@@ -41,7 +42,7 @@ def build(force: bool = False, verbose: bool = False) -> str:
     """Compiles csrc/*.cu into libstairs_b200.so (skipped when up to date).  Returns the path."""
     if not force and not _stale():
         return LIB_PATH
-    jobs = [("engine.cu", []), ("attend.cu", []), ("sample.cu", []), ("paged.cu", [])] + [("forward.cu", ["-DFWD_HD=%d" % hd, "-DFWD_FAM=%d" % fam, "-DFWD_ATT=%d" % att, "-DFWD_ONE=%d" % one, "-DFWD_SHARE=%d" % share])
+    jobs = [("engine.cu", []), ("attend.cu", []), ("sample.cu", []), ("paged.cu", [])] + [("attend_mma.cu", ["-DATT_KS=%d" % ks]) for ks in ATTEND_STEPS] + [("forward.cu", ["-DFWD_HD=%d" % hd, "-DFWD_FAM=%d" % fam, "-DFWD_ATT=%d" % att, "-DFWD_ONE=%d" % one, "-DFWD_SHARE=%d" % share])
                                   for hd, fam, att, one, share in FORWARD]
     log = ""
     failed = False

@@ -6,21 +6,12 @@
 #include <algorithm>
 #include <type_traits>
 
-#include "static_ops.cuh"
+#include "attend.cuh"
 
 namespace stairs {
 namespace {
 
-struct AttendParams {
-  const void* kc; const void* vc; const void* q; void* o;
-  long long page_stride, token_stride, head_stride, q_row, q_head, o_row, o_head;
-  const int* table; const int* row_off; const int* kv_len;
-  int n_req, n_rows, heads, kv_heads, hd, n_pages, page_tokens, max_blocks, max_len;
-  float scale;
-  float* part;                  // partial states of split units
-};
-
-__device__ __forceinline__ int clampi(int v, int lo, int hi) { return v < lo ? lo : (v > hi ? hi : v); }
+using namespace att;
 
 // ------------------------------------------------------------------------------------------------
 // Any type, stride, alignment and head size: one block per row and head, one warp per 32 positions in turn.  Every element is
@@ -104,9 +95,26 @@ template <typename T> __global__ void __launch_bounds__(AP_WARPS * 32) k_attend_
 
 using namespace stairs;
 
+namespace {
+
+// The form that a call takes, by sizes and alignment alone (never by lengths, which the host does not know).
+struct Form { bool vectors; int ks, mg; };
+Form form_of(const stairs_paged* c, int n_heads, int n_req, int n_rows) {
+  Form f{};
+  const int v = 16 / dtype_bytes(c->dtype);
+  f.vectors = c->head_dim % v == 0 && c->page_stride % v == 0 && c->token_stride % v == 0 && c->head_stride % v == 0 && aligned16(c->k_dev) && aligned16(c->v_dev);
+  f.ks = am_ks(c->head_dim);
+  f.mg = am_groups(f.ks, n_rows, n_req, n_heads / c->n_kv_heads);
+  return f;
+}
+
+}  // namespace
+
 extern "C" size_t stairs_attend_workspace_bytes(const stairs_paged* cache, int n_heads, int n_req, int n_rows) {
   if (check_paged("stairs_attend_workspace_bytes", cache)) return 0;
-  return 256;
+  if (n_heads < 1 || n_heads % cache->n_kv_heads || n_req < 1 || n_rows < 1) return 0;
+  const Form f = form_of(cache, n_heads, n_req, n_rows);
+  return f.vectors && cache->dtype != DT_F32 ? am_workspace(f.ks, f.mg, cache->head_dim) : 0;
 }
 
 extern "C" int stairs_attend_static(const stairs_paged* cache, const int32_t* block_table_dev, int max_blocks, int n_req, const int32_t* row_off_dev,
@@ -129,8 +137,26 @@ extern "C" int stairs_attend_static(const stairs_paged* cache, const int32_t* bl
   const int reach = max_blocks * cache->page_tokens;
   AttendParams P{cache->k_dev, cache->v_dev, q_dev, o_dev, cache->page_stride, cache->token_stride, cache->head_stride, q_row_stride, q_head_stride,
                  o_row_stride, o_head_stride, block_table_dev, row_off_dev, kv_len_dev, n_req, n_rows, n_heads, cache->n_kv_heads, cache->head_dim,
-                 cache->n_pages, cache->page_tokens, max_blocks, max_len ? std::min(max_len, reach) : reach, scale, nullptr};
+                 cache->n_pages, cache->page_tokens, max_blocks, max_len ? std::min(max_len, reach) : reach, scale, workspace};
   cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
+  const Form f = form_of(cache, n_heads, n_req, n_rows);
+  const int v = 16 / dtype_bytes(cache->dtype);
+  if (f.vectors && cache->dtype != DT_F32 && aligned16(q_dev) && q_row_stride % v == 0 && q_head_stride % v == 0 && aligned16(o_dev) && o_row_stride % v == 0 &&
+      o_head_stride % v == 0) {
+    const size_t need = am_workspace(f.ks, f.mg, cache->head_dim);
+    if (!workspace || reinterpret_cast<uintptr_t>(workspace) % 256 || workspace_bytes < need)
+      return static_fail(workspace && workspace_bytes < need ? STAIRS_ENOSPC : STAIRS_EINVAL, "%s: %zu bytes of scratch, 256-byte aligned, are needed; %zu at %p were given",
+                         who, need, workspace_bytes, workspace);
+    switch (f.ks) {
+      case 2: return launch_mma<2>(P, cache->dtype, f.mg, st);
+      case 4: return launch_mma<4>(P, cache->dtype, f.mg, st);
+      case 5: return launch_mma<5>(P, cache->dtype, f.mg, st);
+      case 6: return launch_mma<6>(P, cache->dtype, f.mg, st);
+      case 8: return launch_mma<8>(P, cache->dtype, f.mg, st);
+      case 12: return launch_mma<12>(P, cache->dtype, f.mg, st);
+      default: return launch_mma<16>(P, cache->dtype, f.mg, st);
+    }
+  }
   const unsigned blocks = (unsigned)(n_rows * n_heads);
   if (cache->dtype == DT_F32) k_attend_plain<float><<<blocks, AP_WARPS * 32, 0, st>>>(P);
   else if (cache->dtype == DT_BF16) k_attend_plain<bf16><<<blocks, AP_WARPS * 32, 0, st>>>(P);

@@ -1,0 +1,59 @@
+// What the attention kernels on a caller's paged cache share (attend.cu, attend_mma.cu, attend_tc.cu).
+#pragma once
+#include "static_ops.cuh"
+
+namespace stairs {
+namespace att {
+
+struct AttendParams {
+  const void* kc; const void* vc; const void* q; void* o;
+  long long page_stride, token_stride, head_stride, q_row, q_head, o_row, o_head;
+  const int* table; const int* row_off; const int* kv_len;
+  int n_req, n_rows, heads, kv_heads, hd, n_pages, page_tokens, max_blocks, max_len;
+  float scale;
+  void* ws;                     // caller's scratch
+};
+
+__device__ __forceinline__ int clampi(int v, int lo, int hi) { return v < lo ? lo : (v > hi ? hi : v); }
+
+// Request i's rows [first, first + n) and visible length.
+struct Span { int first, n, len; };
+__device__ __forceinline__ Span request_span(const AttendParams& P, int i) {
+  Span s;
+  s.first = max(P.row_off[i], 0);
+  s.n = max(min(P.row_off[i + 1], P.n_rows) - s.first, 0);
+  s.len = clampi(P.kv_len[i], 0, P.max_len);
+  return s;
+}
+
+// --- the split form on mma.sync (attend_mma.cu) -----------------------------------------------------------------
+constexpr int AM_CHUNK = 64;                   // positions per pipeline stage
+constexpr int AM_SMS = 148;
+constexpr int am_pitch(int ks) { return (ks * 2 % 8 == 0 ? ks * 2 : (ks * 2) | 1) * 16; }   // bytes of a staged row of ks 16-element steps
+constexpr int am_smem(int ks, int mg, int nst) {
+  return nst * (2 * AM_CHUNK + 16 * mg) * am_pitch(ks) + (nst + 1) * (AM_CHUNK * 8 + 48) + 8 * 16 * mg * 4 + 64;
+}
+// two CTAs share an SM where three stages and the registers of each fit, else one has as many stages as fit (at most six)
+constexpr int am_ctas(int ks, int mg) { return am_smem(ks, mg, 3) <= 112 * 1024 && (mg == 1 || (mg == 2 && ks <= 6)) ? 2 : 1; }
+constexpr int am_stages(int ks, int mg) {
+  int n = 3;
+  while (n < 6 && am_smem(ks, mg, n + 1) <= (am_ctas(ks, mg) == 2 ? 112 : 226) * 1024) ++n;
+  return n;
+}
+constexpr int am_grid(int ks, int mg) { return AM_SMS * am_ctas(ks, mg); }
+// row groups of 16 queries (rows x heads that share a key head): what the average request fills, and registers and shared memory hold
+constexpr int am_most_groups(int ks) { return ks <= 8 ? 4 : ks <= 12 ? 2 : 1; }
+inline int am_groups(int ks, int n_rows, int n_req, int group) {
+  const long long q = (((long long)n_rows * group + n_req - 1) / n_req + 15) / 16;
+  return (int)(q < 1 ? 1 : q < am_most_groups(ks) ? q : am_most_groups(ks));
+}
+constexpr int am_steps[7] = {2, 4, 5, 6, 8, 12, 16};               // compiled head sizes, in steps of 16
+inline int am_ks(int hd) {
+  for (int k : am_steps) if (hd <= 16 * k) return k;
+  return 16;
+}
+inline size_t am_workspace(int ks, int mg, int hd) { return (size_t)am_grid(ks, mg) * (32 + (size_t)2 * 16 * mg * (hd + 2) * 4); }
+template <int KS> int launch_mma(const AttendParams& P, int dtype, int mg, cudaStream_t st);   // KS: 16-element steps of a head
+
+}  // namespace att
+}  // namespace stairs

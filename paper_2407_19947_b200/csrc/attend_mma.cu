@@ -1,0 +1,509 @@
+// Attention over a caller's paged cache for few queries per key head: 16-bit caches, mma.sync tiles (one object per head size, -DATT_KS).
+//
+// Bound by reading K and V: a call's (request, 64-position chunk, key head, block of queries) steps form one list, cut evenly over all CTAs
+// whatever the requests' lengths are, and every CTA streams its part through a ring of shared-memory stages with 16-byte asynchronous copies
+// (16-byte copies because a cache has any strides, page sizes down to one token, and no tensor map is needed).
+// The queries of a unit - rows x heads that share the key head, 16 per row group - meet each stage together, so K and V
+// are read from memory once.  Within a CTA four warps per row group take 16 of a chunk's 64 positions each, with a softmax state of
+// their own, so nothing is exchanged until a unit's part ends.  Parts of units cut over CTAs go to the caller's scratch and are
+// joined by a second, short kernel, in the order of the positions: results do not depend on timing.
+#include <type_traits>
+
+#include "attend.cuh"
+
+namespace stairs {
+namespace att {
+namespace {
+
+__device__ __forceinline__ void cp16(uint32_t dst, const void* src, bool on) {   // zeros where off
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(on ? 16 : 0) : "memory");
+}
+__device__ __forceinline__ void cp_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N> __device__ __forceinline__ void cp_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
+__device__ __forceinline__ void ldm4(uint32_t at, uint32_t* r) {
+  asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0, %1, %2, %3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(at) : "memory");
+}
+__device__ __forceinline__ void ldm4t(uint32_t at, uint32_t* r) {
+  asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0, %1, %2, %3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(at) : "memory");
+}
+template <typename T> __device__ __forceinline__ void mma16816(float* c, const uint32_t* a, uint32_t b0, uint32_t b1) {
+  if (std::is_same<T, bf16>::value)
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+                 : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+  else
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+                 : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+template <typename T> __device__ __forceinline__ uint32_t pack2(float lo, float hi) {
+  uint32_t r;
+  if (std::is_same<T, bf16>::value) asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+  else asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+  return r;
+}
+__device__ __forceinline__ float ex2(float x) { return exp2f(x); }
+
+// One step of the list, filed for the copies and the computation behind it.
+struct Step {
+  int first, n, len, qb, h, chunk;      // request's rows and length, block of queries, key head, chunk of positions
+  int begins, ends;                     // first step of this CTA's part of the unit; 1: last one, 2: last one and the unit is cut
+  int slot;                             // where a cut part goes
+  unsigned valid[2];                    // positions of the chunk whose page is one
+};
+
+template <int KS, int MG> struct Geo {
+  static constexpr int NC = MG * 128, NT = NC + 64, ROWS = MG * 16, PC = KS * 2, HD = KS * 16, NST = am_stages(KS, MG);   // NC computing threads, 64 that copy
+  static constexpr bool XOR = PC % 8 == 0;                        // 16-byte pieces permuted within a row, else an odd pitch: no bank conflicts
+  static constexpr int PITCH = am_pitch(KS);
+  static constexpr int KV = AM_CHUNK * PITCH, STAGE = 2 * KV, QB = ROWS * PITCH, R = NST + 1;
+  static constexpr int MERGE_MAX = STAGE / (4 * ROWS * 4) / 8 * 8, MC = MERGE_MAX < HD ? MERGE_MAX : HD;   // columns merged at a time
+  static constexpr int SMEM = am_smem(KS, MG, NST);
+  static_assert(sizeof(Step) <= 48 && SMEM <= 227 * 1024, "shared memory");
+  static __device__ __forceinline__ uint32_t at(int row, int piece) { return row * PITCH + ((XOR ? piece ^ (row & 7) : piece) << 4); }
+};
+
+struct Meta { int parts, slot, first, n, qb, h, pad0, pad1; };   // of the unit that a CTA begins and does not end
+
+template <typename T, int KS, int MG>
+__global__ void __launch_bounds__(MG * 128 + 64, am_ctas(KS, MG)) k_attend_mma(const __grid_constant__ AttendParams P) {
+  typedef Geo<KS, MG> G;
+  constexpr int NST = G::NST;
+  extern __shared__ __align__(128) unsigned char am_sm[];
+  unsigned char* qring = am_sm + NST * G::STAGE;
+  long long* roff = reinterpret_cast<long long*>(qring + NST * G::QB);            // [R][64] element offset of each position's row
+  Step* steps = reinterpret_cast<Step*>(roff + G::R * AM_CHUNK);                  // [R]
+  float* xm = reinterpret_cast<float*>(steps + G::R);                             // [4][ROWS] maxima, then sums
+  float* xl = xm + 4 * G::ROWS;
+  __shared__ long long w_sum[G::NT / 32];
+  __shared__ int s_req;
+  __shared__ long long s_rem;
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, pw = warp & 3, mg = warp >> 2;
+  const int group = P.heads / P.kv_heads;
+  launch_dependents();
+  wait_prerequisites();
+
+  // this CTA's part of the list
+  auto steps_of = [&](const Span& s, int& chunks) -> long long {
+    chunks = max(1, (s.len + AM_CHUNK - 1) / AM_CHUNK);
+    return s.n ? ((long long)s.n * group + G::ROWS - 1) / G::ROWS * P.kv_heads * chunks : 0;
+  };
+  auto scan = [&](long long v, long long& total) {
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const long long u = __shfl_up_sync(0xffffffffu, v, o);
+      if (lane >= o) v += u;
+    }
+    __syncthreads();
+    if (lane == 31) w_sum[warp] = v;
+    __syncthreads();
+    long long before = 0, all = 0;
+#pragma unroll
+    for (int w = 0; w < G::NT / 32; ++w) { if (w < warp) before += w_sum[w]; all += w_sum[w]; }
+    total = all;
+    return v + before;
+  };
+  long long total = 0, mine_incl = 0, mine = 0;
+  for (int base = 0; base < P.n_req; base += G::NT) {
+    int chunks;
+    mine = base + tid < P.n_req ? steps_of(request_span(P, base + tid), chunks) : 0;
+    long long all;
+    mine_incl = scan(mine, all) + total;
+    total += all;
+  }
+  const long long parts_all = min((long long)gridDim.x, total);    // CTAs with a part: each has a step at least
+  Meta* meta = reinterpret_cast<Meta*>(P.ws) + blockIdx.x;
+  if (blockIdx.x >= parts_all) {
+    if (tid == 0) meta->parts = 0;
+    return;
+  }
+  const long long x0 = total * blockIdx.x / parts_all, x1 = total * (blockIdx.x + 1) / parts_all;
+  if (P.n_req <= G::NT) {
+    if (x0 >= mine_incl - mine && x0 < mine_incl) { s_req = tid; s_rem = x0 - (mine_incl - mine); }
+  } else {
+    long long before = 0;
+    for (int base = 0; base < P.n_req; base += G::NT) {
+      int chunks;
+      const long long v = base + tid < P.n_req ? steps_of(request_span(P, base + tid), chunks) : 0;
+      long long all;
+      const long long incl = scan(v, all) + before;
+      if (x0 >= incl - v && x0 < incl) { s_req = base + tid; s_rem = x0 - (incl - v); }
+      before += all;
+    }
+  }
+  __syncthreads();
+  const int n_steps = (int)min(x1 - x0, 0x7fffffffll);
+
+  const uint32_t sm0 = smem_addr(am_sm), q0 = smem_addr(qring);
+  if (warp >= MG * 4) {
+    // ---------------------------------------------------------------- two warps that walk the list and copy, one thread per position
+    const int ct = tid - G::NC;
+    int req = s_req, chunks, unit, chunk;
+    Span sp = request_span(P, req);
+    int units = (int)(steps_of(sp, chunks) / chunks);
+    unit = (int)(s_rem / chunks); chunk = (int)(s_rem - (long long)unit * chunks);
+    int seg = 0, part_begin = chunk, planned = 0;
+    Step plan;                                  // the step being planned, and this thread's position's place
+    long long place = -1;
+    auto plan_load = [&]() {                    // step `planned` (its table entry is on the way when this returns)
+      if (planned >= n_steps) return;
+      plan.first = sp.first; plan.n = sp.n; plan.len = sp.len;
+      plan.qb = unit / P.kv_heads; plan.h = unit - plan.qb * P.kv_heads; plan.chunk = chunk;
+      plan.begins = chunk == part_begin;
+      const bool unit_ends = chunk + 1 == chunks, last = planned + 1 == n_steps;
+      plan.ends = (unit_ends || last) ? ((part_begin > 0 || !unit_ends) ? 2 : 1) : 0;
+      plan.slot = 2 * blockIdx.x + (seg ? 1 : 0);
+      const int p = chunk * AM_CHUNK + ct;
+      place = -1;
+      if (p < sp.len) {
+        const int b = p / P.page_tokens, page = __ldg(P.table + (size_t)req * P.max_blocks + b);
+        if (page >= 0 && page < P.n_pages) place = page * P.page_stride + (p - b * P.page_tokens) * P.token_stride;
+      }
+      if (last && ct == 0) {
+        Meta m{};
+        if (plan.ends == 2 && part_begin == 0) {                       // the unit goes on in the next CTAs
+          // the CTA that holds the unit's last step: the first whose part ends behind it
+          const long long end = x1 + (chunks - 1 - chunk);             // one past the unit's last step
+          long long e = (end * parts_all - 1) / total;                 // (about; corrected below)
+          while (e > 0 && total * e / parts_all >= end) --e;
+          while (total * (e + 1) / parts_all < end) ++e;
+          m.parts = (int)(e - blockIdx.x) + 1;
+          m.slot = plan.slot; m.first = sp.first; m.n = sp.n; m.qb = plan.qb; m.h = plan.h;
+        }
+        *meta = m;
+      }
+      if (unit_ends) {
+        chunk = 0; ++seg; part_begin = 0;
+        if (++unit == units && !last) {
+          unit = 0;
+          do { sp = request_span(P, ++req); } while (sp.n == 0);       // (there are steps left, so there is such a request)
+          units = (int)(steps_of(sp, chunks) / chunks);
+        }
+      } else ++chunk;
+    };
+    auto plan_store = [&]() {
+      if (planned < n_steps) {
+        const int slot = planned % G::R;
+        roff[slot * AM_CHUNK + ct] = place;
+        const unsigned v = __ballot_sync(0xffffffffu, place >= 0);
+        Step* s = steps + slot;
+        if (lane == 0) s->valid[ct >> 5] = v;
+        if (ct == 0) {
+          s->first = plan.first; s->n = plan.n; s->len = plan.len; s->qb = plan.qb; s->h = plan.h; s->chunk = plan.chunk;
+          s->begins = plan.begins; s->ends = plan.ends; s->slot = plan.slot;
+        }
+        ++planned;
+      }
+    };
+    const int pieces = P.hd / 8;                // 16-byte pieces of a head that exist
+    int loaded_units = 0;
+    auto issue = [&](int x) {                   // copies of step x into its stage
+      if (x < n_steps) {
+        const Step& s = steps[x % G::R];
+        const long long* ro = roff + (x % G::R) * AM_CHUNK;
+        const uint32_t dst = sm0 + (x % NST) * G::STAGE;
+        const T* kb = reinterpret_cast<const T*>(P.kc) + s.h * P.head_stride;
+        const T* vb = reinterpret_cast<const T*>(P.vc) + s.h * P.head_stride;
+#pragma unroll 8
+        for (int i = 0; i < G::PC; ++i) {
+          const int it = i * AM_CHUNK + ct, r = it / G::PC, c = it % G::PC;
+          const long long ro_r = ro[r];
+          const bool on = ro_r >= 0 && c < pieces;
+          const long long src = on ? ro_r + c * 8 : 0;
+          cp16(dst + G::at(r, c), kb + src, on);
+          cp16(dst + G::KV + G::at(r, c), vb + src, on);
+        }
+        if (s.begins) {
+          const uint32_t qd = q0 + (loaded_units % NST) * G::QB;
+          for (int it = ct; it < G::ROWS * G::PC; it += 64) {
+            const int r = it / G::PC, c = it % G::PC, qi = s.qb * G::ROWS + r, j = qi / group;
+            const bool on = j < s.n && c < pieces;
+            const T* src = reinterpret_cast<const T*>(P.q) + (on ? (s.first + j) * P.q_row + (s.h * group + qi - j * group) * P.q_head + c * 8 : 0);
+            cp16(qd + G::at(r, c), src, on);
+          }
+          ++loaded_units;
+        }
+      }
+      cp_commit();
+    };
+    auto copiers_sync = []() { asm volatile("bar.sync 2, 64;" ::: "memory"); };
+    for (int i = 0; i < NST; ++i) { plan_load(); plan_store(); }
+    copiers_sync();
+    for (int i = 0; i < NST - 1; ++i) issue(i);
+    for (int x = 0; x < n_steps; ++x) {
+      cp_wait<NST - 2>();
+      __syncthreads();                          // step x has arrived; its predecessor's stage and entry are free
+      issue(x + NST - 1);
+      plan_load();
+      plan_store();
+    }
+    cp_wait<0>();
+    return;
+  }
+
+  // ------------------------------------------------------------------ computing warps
+  const float sc = P.scale * 1.4426950408889634f;                  // exponentials in base 2
+  auto group_sync = []() { asm volatile("bar.sync 1, %0;" ::"n"(MG * 128) : "memory"); };
+  float acc[KS * 2][4], m_run[2], l_run[2];
+  int cur_unit = -1, last0 = 0, last1 = 0;
+  for (int x = 0; x < n_steps; ++x) {
+    __syncthreads();
+    const Step& s = steps[x % G::R];
+    const int s_first = s.first, s_n = s.n, s_len = s.len, s_qb = s.qb, s_h = s.h, s_ends = s.ends, s_slot = s.slot;
+    const int r0 = mg * 16 + (lane >> 2), qi0 = s_qb * G::ROWS + r0, qi1 = qi0 + 8;
+    if (s.begins) {
+      ++cur_unit;
+#pragma unroll
+      for (int i = 0; i < KS * 2; ++i)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) acc[i][j] = 0.f;
+      m_run[0] = m_run[1] = -INFINITY; l_run[0] = l_run[1] = 0.f;
+      // the last position that this thread's two queries see
+      const int j0 = qi0 / group, j1 = qi1 / group;
+      last0 = j0 < s_n ? s_len - s_n + j0 : -1;
+      last1 = j1 < s_n ? s_len - s_n + j1 : -1;
+    }
+    const uint32_t ks = sm0 + (x % NST) * G::STAGE, vs = ks + G::KV, qs = q0 + (cur_unit % NST) * G::QB;
+    const int p0 = s.chunk * AM_CHUNK + pw * 16;                   // this warp's 16 positions
+    const unsigned valid = (s.valid[pw >> 1] >> ((pw & 1) * 16)) & 0xffffu;
+    const int seen_by_all = s_len - s_n + (s_qb * G::ROWS + mg * 16) / group;   // the first query's last position
+    const int sub = lane & 7, mat = lane >> 3;
+    if (valid) {                                                   // (else nothing is added)
+      float sr[2][4];
+#pragma unroll
+      for (int i = 0; i < 2; ++i)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) sr[i][j] = 0.f;
+#pragma unroll
+      for (int k = 0; k < KS; ++k) {
+        uint32_t a[4], b[4];
+        ldm4(qs + G::at(mg * 16 + sub + (mat & 1) * 8, k * 2 + (mat >> 1)), a);
+        ldm4(ks + G::at(pw * 16 + sub + (mat >> 1) * 8, k * 2 + (mat & 1)), b);
+        mma16816<T>(sr[0], a, b[0], b[1]);
+        mma16816<T>(sr[1], a, b[2], b[3]);
+      }
+      const bool edge = valid != 0xffffu || p0 + 15 > seen_by_all;
+      float mx0 = -INFINITY, mx1 = -INFINITY;
+#pragma unroll
+      for (int i = 0; i < 2; ++i)
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          const int pl = i * 8 + (lane & 3) * 2 + e;
+          float u = sr[i][e] * sc, w = sr[i][2 + e] * sc;
+          if (edge) {
+            const bool ok = (valid >> pl) & 1u;
+            if (!ok || p0 + pl > last0) u = -INFINITY;
+            if (!ok || p0 + pl > last1) w = -INFINITY;
+          }
+          sr[i][e] = u; sr[i][2 + e] = w;
+          mx0 = fmaxf(mx0, u); mx1 = fmaxf(mx1, w);
+        }
+      mx0 = fmaxf(mx0, __shfl_xor_sync(0xffffffffu, mx0, 1)); mx0 = fmaxf(mx0, __shfl_xor_sync(0xffffffffu, mx0, 2));
+      mx1 = fmaxf(mx1, __shfl_xor_sync(0xffffffffu, mx1, 1)); mx1 = fmaxf(mx1, __shfl_xor_sync(0xffffffffu, mx1, 2));
+      const float n0 = fmaxf(m_run[0], mx0), n1 = fmaxf(m_run[1], mx1);
+      const float f0 = n0 == -INFINITY ? 0.f : n0, f1 = n1 == -INFINITY ? 0.f : n1;
+      const float c0 = ex2(m_run[0] - f0), c1 = ex2(m_run[1] - f1);
+      m_run[0] = n0; m_run[1] = n1;
+      l_run[0] *= c0; l_run[1] *= c1;
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          sr[i][e] = ex2(sr[i][e] - f0); sr[i][2 + e] = ex2(sr[i][2 + e] - f1);
+          l_run[0] += sr[i][e]; l_run[1] += sr[i][2 + e];
+        }
+      }
+      if (__any_sync(0xffffffffu, c0 != 1.f || c1 != 1.f)) {
+#pragma unroll
+        for (int i = 0; i < KS * 2; ++i) { acc[i][0] *= c0; acc[i][1] *= c0; acc[i][2] *= c1; acc[i][3] *= c1; }
+      }
+      // Where some of these positions are hidden from some rows, an infinity or NaN among their values would reach those
+      // rows as 0 * infinity in the matrix product: looked for, left out of the product, and added for the rows that see it.
+      constexpr uint32_t EXPO = std::is_same<T, bf16>::value ? 0x7f80u : 0x7c00u;
+      bool odd = false;
+      if (p0 + 15 > seen_by_all) {
+        for (int it = lane; it < 16 * G::PC; it += 32) {
+          const uint32_t at = vs + G::at(pw * 16 + it / G::PC, it % G::PC);
+          uint32_t w[4];
+          asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]) : "r"(at) : "memory");
+#pragma unroll
+          for (int e = 0; e < 4; ++e) odd = odd || (w[e] & EXPO) == EXPO || ((w[e] >> 16) & EXPO) == EXPO;
+        }
+        odd = __any_sync(0xffffffffu, odd);
+      }
+      uint32_t a[4];   // the weights, rounded to the cache's type: the matrix product takes them so
+      a[0] = pack2<T>(sr[0][0], sr[0][1]); a[1] = pack2<T>(sr[0][2], sr[0][3]);
+      a[2] = pack2<T>(sr[1][0], sr[1][1]); a[3] = pack2<T>(sr[1][2], sr[1][3]);
+#pragma unroll
+      for (int d = 0; d < KS; ++d) {
+        uint32_t b[4];
+        ldm4t(vs + G::at(pw * 16 + sub + (mat & 1) * 8, d * 2 + (mat >> 1)), b);
+        if (odd) {
+#pragma unroll
+          for (int e = 0; e < 4; ++e) b[e] &= ((b[e] & EXPO) == EXPO ? 0u : 0xffffu) | (((b[e] >> 16) & EXPO) == EXPO ? 0u : 0xffff0000u);
+        }
+        mma16816<T>(acc[2 * d], a, b[0], b[1]);
+        mma16816<T>(acc[2 * d + 1], a, b[2], b[3]);
+      }
+      if (odd) {
+        const unsigned char* vrow = am_sm + (x % NST) * G::STAGE + G::KV;
+        for (int pl = 0; pl < 16; ++pl) {
+          const bool ok = (valid >> pl) & 1u, see0 = ok && p0 + pl <= last0, see1 = ok && p0 + pl <= last1;
+#pragma unroll
+          for (int d = 0; d < KS * 2; ++d) {
+            const T* v = reinterpret_cast<const T*>(vrow + G::at(pw * 16 + pl, d)) + (lane & 3) * 2;
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+              const float y = to_f32(v[e]);
+              if (isfinite(y)) continue;
+              if (see0) acc[d][e] += y;
+              if (see1) acc[d][2 + e] += y;
+            }
+          }
+        }
+      }
+    }
+    if (s_ends) {
+      // the four warps of a row group: common maximum, then sums, through the stage just consumed
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        l_run[e] += __shfl_xor_sync(0xffffffffu, l_run[e], 1);
+        l_run[e] += __shfl_xor_sync(0xffffffffu, l_run[e], 2);
+      }
+      if ((lane & 3) == 0) {
+        xm[pw * G::ROWS + r0] = m_run[0]; xm[pw * G::ROWS + r0 + 8] = m_run[1];
+        xl[pw * G::ROWS + r0] = l_run[0]; xl[pw * G::ROWS + r0 + 8] = l_run[1];
+      }
+      group_sync();
+      float f[2];
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        float M = -INFINITY;
+#pragma unroll
+        for (int w = 0; w < 4; ++w) M = fmaxf(M, xm[w * G::ROWS + r0 + 8 * e]);
+        f[e] = m_run[e] == -INFINITY ? 0.f : ex2(m_run[e] - M);
+      }
+      float* mt = reinterpret_cast<float*>(am_sm + (x % NST) * G::STAGE);          // [4][ROWS][MC]
+      float* part = reinterpret_cast<float*>(reinterpret_cast<unsigned char*>(P.ws) + (size_t)gridDim.x * sizeof(Meta)) + s_slot * (size_t)(G::ROWS * (P.hd + 2));
+      for (int col0 = 0; col0 < P.hd; col0 += G::MC) {
+#pragma unroll
+        for (int d = 0; d < KS * 2; ++d) {
+          const int col = d * 8 + (lane & 3) * 2 - col0;
+          if (col >= 0 && col < G::MC) {
+            float* at0 = mt + ((size_t)pw * G::ROWS + r0) * G::MC + col;
+            *reinterpret_cast<float2*>(at0) = make_float2(f[0] != 0.f ? acc[d][0] * f[0] : 0.f, f[0] != 0.f ? acc[d][1] * f[0] : 0.f);
+            *reinterpret_cast<float2*>(at0 + 8 * G::MC) = make_float2(f[1] != 0.f ? acc[d][2] * f[1] : 0.f, f[1] != 0.f ? acc[d][3] * f[1] : 0.f);
+          }
+        }
+        group_sync();
+        const int cols = min(G::MC, P.hd - col0);                  // (both are multiples of 8)
+        for (int it = tid; it < G::ROWS * (G::MC / 4); it += G::NC) {
+          const int r = it / (G::MC / 4), c = it % (G::MC / 4) * 4, qi = s_qb * G::ROWS + r, j = qi / group;
+          if (c >= cols || j >= s_n) continue;
+          float M = -INFINITY, L = 0.f;
+#pragma unroll
+          for (int w = 0; w < 4; ++w) M = fmaxf(M, xm[w * G::ROWS + r]);
+#pragma unroll
+          for (int w = 0; w < 4; ++w) { const float mw = xm[w * G::ROWS + r]; L += mw == -INFINITY ? 0.f : xl[w * G::ROWS + r] * ex2(mw - M); }
+          float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+          for (int w = 0; w < 4; ++w) {
+            const float4 v = *reinterpret_cast<const float4*>(mt + ((size_t)w * G::ROWS + r) * G::MC + c);
+            o.x += v.x; o.y += v.y; o.z += v.z; o.w += v.w;
+          }
+          if (s_ends == 2) {
+            *reinterpret_cast<float4*>(part + (size_t)r * P.hd + col0 + c) = o;
+            if (c == 0 && col0 == 0) { part[(size_t)G::ROWS * P.hd + r] = M; part[(size_t)G::ROWS * (P.hd + 1) + r] = L; }
+          } else {
+            const float inv = M == -INFINITY ? 0.f : 1.f / L;
+            T* dst = reinterpret_cast<T*>(P.o) + (s_first + j) * P.o_row + (s_h * group + qi - j * group) * P.o_head + col0 + c;
+            uint2 u;
+            u.x = pack2<T>(o.x * inv, o.y * inv); u.y = pack2<T>(o.z * inv, o.w * inv);
+            *reinterpret_cast<uint2*>(dst) = u;
+          }
+        }
+        group_sync();
+      }
+    }
+  }
+}
+
+// Joins the parts of the unit that CTA blockIdx.x of the kernel above began and did not end: part 0 is where that CTA says,
+// the next ones are the first parts of the CTAs behind it.
+template <typename T, int MG> __global__ void __launch_bounds__(128) k_attend_join(const __grid_constant__ AttendParams P) {
+  constexpr int ROWS = MG * 16;
+  __shared__ float sM[ROWS], sInv[ROWS];
+  wait_prerequisites();
+  const Meta m = *(reinterpret_cast<const Meta*>(P.ws) + blockIdx.x);
+  if (m.parts == 0) return;
+  const int group = P.heads / P.kv_heads, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const size_t slot = (size_t)ROWS * (P.hd + 2);
+  const float* base = reinterpret_cast<const float*>(reinterpret_cast<const unsigned char*>(P.ws) + (size_t)gridDim.x * sizeof(Meta));
+  auto part = [&](int p) { return base + (p ? 2 * (blockIdx.x + p) : m.slot) * slot; };
+  const int rows = min(ROWS, m.n * group - m.qb * ROWS);
+  // this block's rows (grid y)
+  const int per = (rows + gridDim.y - 1) / gridDim.y, ra = blockIdx.y * per, rb = min(rows, ra + per);
+  for (int r = ra + warp; r < rb; r += 4) {
+    float M = -INFINITY, L = 0.f;
+    for (int p = lane; p < m.parts; p += 32) {
+      const float* s = part(p) + (size_t)ROWS * P.hd;
+      const float mp = s[r], lp = s[ROWS + r], n = fmaxf(M, mp);
+      if (n != -INFINITY) L = L * ex2(M - n) + lp * ex2(mp - n);
+      M = n;
+    }
+    const float mx = warp_max(M);
+    L = warp_sum(M == -INFINITY ? 0.f : L * ex2(M - mx));
+    if (lane == 0) { sM[r] = mx; sInv[r] = mx == -INFINITY ? 0.f : 1.f / L; }
+  }
+  __syncthreads();
+  const int q4 = P.hd / 4;
+  for (int it = threadIdx.x; it < (rb - ra) * q4; it += 128) {
+    const int r = ra + it / q4, c = it % q4 * 4, qi = m.qb * ROWS + r, j = qi / group;
+    const float M = sM[r], inv = sInv[r];
+    float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 4
+    for (int p = 0; p < m.parts; ++p) {
+      const float* s = part(p);
+      const float mp = s[(size_t)ROWS * P.hd + r];
+      const float4 v = *reinterpret_cast<const float4*>(s + (size_t)r * P.hd + c);
+      const float w = mp == -INFINITY ? 0.f : ex2(mp - M);
+      if (w != 0.f) { o.x = fmaf(v.x, w, o.x); o.y = fmaf(v.y, w, o.y); o.z = fmaf(v.z, w, o.z); o.w = fmaf(v.w, w, o.w); }
+    }
+    T* dst = reinterpret_cast<T*>(P.o) + (m.first + j) * P.o_row + (m.h * group + qi - j * group) * P.o_head + c;
+    uint2 u;
+    u.x = pack2<T>(o.x * inv, o.y * inv); u.y = pack2<T>(o.z * inv, o.w * inv);
+    *reinterpret_cast<uint2*>(dst) = u;
+  }
+}
+
+template <typename T, int KS, int MG> int launch(const AttendParams& P, cudaStream_t st) {
+  typedef Geo<KS, MG> G;
+  auto kern = k_attend_mma<T, KS, MG>;
+  if (G::SMEM > 48 * 1024) SCK(cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, G::SMEM));
+  kern<<<am_grid(KS, MG), G::NT, G::SMEM, st>>>(P);
+  SCK(cudaGetLastError());
+  cudaLaunchConfig_t cfg{};
+  cfg.gridDim = dim3(am_grid(KS, MG), 4); cfg.blockDim = dim3(128); cfg.stream = st;
+  cudaLaunchAttribute at[1];
+  at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization; at[0].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = at; cfg.numAttrs = 1;
+  SCK(cudaLaunchKernelEx(&cfg, k_attend_join<T, MG>, P));
+  return STAIRS_OK;
+}
+
+template <typename T> int launch_mg(const AttendParams& P, int mg, cudaStream_t st) {
+  if constexpr (am_most_groups(ATT_KS) >= 4) {
+    if (mg == 4) return launch<T, ATT_KS, 4>(P, st);
+    if (mg == 3) return launch<T, ATT_KS, 3>(P, st);
+  }
+  if constexpr (am_most_groups(ATT_KS) >= 2)
+    if (mg == 2) return launch<T, ATT_KS, 2>(P, st);
+  return launch<T, ATT_KS, 1>(P, st);
+}
+
+}  // namespace
+
+template <> int launch_mma<ATT_KS>(const AttendParams& P, int dtype, int mg, cudaStream_t st) {
+  return dtype == DT_BF16 ? launch_mg<bf16>(P, mg, st) : launch_mg<__half>(P, mg, st);
+}
+
+}  // namespace att
+}  // namespace stairs

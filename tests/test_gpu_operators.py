@@ -146,11 +146,12 @@ class Paged:
         self.g = g
 
 
-def check_attend(st, p, q, new, lens, scale=None, slack=0, max_len=0):
+def check_attend(st, p, q, new, lens, scale=None, slack=0, max_len=0, out=None):
     rows = sum(new)
     off, kv = i32(np.concatenate([[0], np.cumsum(new)]).tolist()), i32(lens)
     mark = 7.25
-    out = torch.full((rows + slack, q.shape[1], q.shape[2]), mark, dtype=q.dtype, device=DEV)
+    if out is None:
+        out = torch.full((rows + slack, q.shape[1], q.shape[2]), mark, dtype=q.dtype, device=DEV)
     s = scale if scale is not None else q.shape[2] ** -0.5
     padded = torch.cat([q, q[:slack]])                                   # (slack: rows behind the last request's)
     got = st.attend_static(padded if slack else q, p.k, p.v, p.table, off, kv, scale=scale, out=out, max_len=max_len)
@@ -259,12 +260,11 @@ def test_attend_strides_and_alignment(st, dtype):
         p = Paged(6, d, 2, 64, 16, [50, 9], shift=shift)
         big = torch.randn((12, 3, 8, 64 + shift), generator=p.g, device=DEV).to(d)
         q = big[:, 1, :, shift:]                                         # rows of a wider projection, at an odd address
-        want = check_attend(st, p, q, [8, 4], [50, 9])
-        out = torch.full((12, 64, 16), 3.0, dtype=d, device=DEV).transpose(1, 2)[:, ::2]
-        store = torch.full((12, 16, 65), 3.0, dtype=d, device=DEV)
-        out = store[:, ::2, 1:]
-        st.attend_static(q, p.k, p.v, p.table, i32([0, 8, 12]), i32([50, 9]), out=out)
-        assert torch.equal(out, want) and bool((store[:, 1::2] == 3).all()) and bool((store[:, :, 0] == 3).all())
+        check_attend(st, p, q, [8, 4], [50, 9])
+        for width, at in ((65, 1), (72, 8)):                             # results at odd addresses, and with gaps between heads
+            store = torch.full((12, 16, width), 3.0, dtype=d, device=DEV)
+            check_attend(st, p, q, [8, 4], [50, 9], out=store[:, ::2, at:])
+            assert bool((store[:, 1::2] == 3).all()) and bool((store[:, :, :at] == 3).all())
 
 
 def test_attend_offsets_beyond_32_bits(st):
