@@ -98,13 +98,14 @@ using namespace stairs;
 namespace {
 
 // The form that a call takes, by sizes and alignment alone (never by lengths, which the host does not know).
-struct Form { bool vectors; int ks, mg; };
+struct Form { bool vectors, tc; int ks, mg; };
 Form form_of(const stairs_paged* c, int n_heads, int n_req, int n_rows) {
   Form f{};
   const int v = 16 / dtype_bytes(c->dtype);
   f.vectors = c->head_dim % v == 0 && c->page_stride % v == 0 && c->token_stride % v == 0 && c->head_stride % v == 0 && aligned16(c->k_dev) && aligned16(c->v_dev);
   f.ks = am_ks(c->head_dim);
   f.mg = am_groups(f.ks, n_rows, n_req, n_heads / c->n_kv_heads);
+  f.tc = f.vectors && c->dtype != DT_F32 && (long long)n_rows * (n_heads / c->n_kv_heads) > 64ll * n_req && tc_takes(c, 1.f);
   return f;
 }
 
@@ -114,7 +115,9 @@ extern "C" size_t stairs_attend_workspace_bytes(const stairs_paged* cache, int n
   if (check_paged("stairs_attend_workspace_bytes", cache)) return 0;
   if (n_heads < 1 || n_heads % cache->n_kv_heads || n_req < 1 || n_rows < 1) return 0;
   const Form f = form_of(cache, n_heads, n_req, n_rows);
-  return f.vectors && cache->dtype != DT_F32 ? am_workspace(f.ks, f.mg, cache->head_dim) : 0;
+  if (!f.vectors || cache->dtype == DT_F32) return 0;
+  const size_t mma = am_workspace(f.ks, f.mg, cache->head_dim);
+  return f.tc ? std::max(mma, tc_workspace(cache->head_dim)) : mma;
 }
 
 extern "C" int stairs_attend_static(const stairs_paged* cache, const int32_t* block_table_dev, int max_blocks, int n_req, const int32_t* row_off_dev,
@@ -143,10 +146,12 @@ extern "C" int stairs_attend_static(const stairs_paged* cache, const int32_t* bl
   const int v = 16 / dtype_bytes(cache->dtype);
   if (f.vectors && cache->dtype != DT_F32 && aligned16(q_dev) && q_row_stride % v == 0 && q_head_stride % v == 0 && aligned16(o_dev) && o_row_stride % v == 0 &&
       o_head_stride % v == 0) {
-    const size_t need = am_workspace(f.ks, f.mg, cache->head_dim);
+    const bool tc = f.tc && scale > 0.f;
+    const size_t need = tc ? tc_workspace(cache->head_dim) : am_workspace(f.ks, f.mg, cache->head_dim);
     if (!workspace || reinterpret_cast<uintptr_t>(workspace) % 256 || workspace_bytes < need)
       return static_fail(workspace && workspace_bytes < need ? STAIRS_ENOSPC : STAIRS_EINVAL, "%s: %zu bytes of scratch, 256-byte aligned, are needed; %zu at %p were given",
                          who, need, workspace_bytes, workspace);
+    if (tc) return launch_tc(P, cache->dtype, st);
     switch (f.ks) {
       case 2: return launch_mma<2>(P, cache->dtype, f.mg, st);
       case 4: return launch_mma<4>(P, cache->dtype, f.mg, st);

@@ -55,5 +55,10 @@ inline int am_ks(int hd) {
 inline size_t am_workspace(int ks, int mg, int hd) { return (size_t)am_grid(ks, mg) * (32 + (size_t)2 * 16 * mg * (hd + 2) * 4); }
 template <int KS> int launch_mma(const AttendParams& P, int dtype, int mg, cudaStream_t st);   // KS: 16-element steps of a head
 
+// --- many queries per key head on tcgen05 (attend_tc.cu) --------------------------------------------------------
+bool tc_takes(const stairs_paged* c, float scale);
+size_t tc_workspace(int hd);
+int launch_tc(const AttendParams& P, int dtype, cudaStream_t st);
+
 }  // namespace att
 }  // namespace stairs

@@ -1,0 +1,625 @@
+// Attention over a caller's paged cache for many queries per key head (prompt chunks): 16-bit caches, heads of up to 128, tcgen05.
+//
+// Bound by the tensor pipe and, as closely, by the exponentials: 128 x 128 scores cost an SM 256 cycles of each of the two products
+// and 1024 of its special-function units.  So a CTA works on two tiles of 128 queries at a time: while one tile's softmax runs, the other's products do.
+//   S = Q.K^T (M = N = 128) -> TMEM; one thread per query takes its row into registers, writes the weights back over it as 16-bit
+//   values, and O += P.V takes them from there as the A operand, V as copied (positions are the MMA's K, so V is MN-major).
+// TMEM: S of two tiles (128 columns each) and O of two tiles: all 512 columns, one CTA per SM.
+// Warps: 0-3 and 4-7 softmax of a tile each, 8 K/V copies (tiled TMA, one box per page slice and 64 columns; pages that are none lie
+// outside the tensor and arrive as zeros), 9 MMA issue and TMEM, 10-11 queries (16-byte asynchronous copies: any strides) and the values of chunks that
+// reach past some query's last position: what lies behind the request's end is cleared, and infinities and NaN are taken out, since
+// 0 * infinity in a product would carry them to rows that do not see them; rows that do get them added at the end.
+// The steps (request, 256 queries, key head, 128 positions; only visible ones) form one list, cut evenly over the CTAs; units cut over
+// CTAs are joined by a second kernel.
+#include <cuda.h>
+
+#include <type_traits>
+
+#include "attend_join.cuh"
+#include "gemm_tc.cuh"
+
+namespace stairs {
+namespace att {
+namespace {
+
+using namespace tc;
+
+constexpr int AT_CH = 128, AT_THREADS = 384, AT_ROWS = 256, AT_STAGES = 2, AT_RING = 4;
+constexpr unsigned long long AT_WAIT = 4000000000ull;   // cycles (two seconds) after which a wait gives up
+
+struct TcParams {
+  CUtensorMap kmap, vmap;       // [page][head or token][token or head][64 columns]; box: one page slice of one head
+  AttendParams a;
+  int box_rows, heads_outer;    // heads_outer: the head is the third coordinate, the token the second
+};
+
+template <bool BF> __device__ __forceinline__ uint32_t instr_desc(int n, int b_mn_major) {   // fp32 accumulator, A and B of one 16-bit type, M = 128
+  return (1u << 4) | (BF ? (1u << 7) | (1u << 10) : 0u) | ((uint32_t)b_mn_major << 16) | ((uint32_t)(n >> 3) << 17) | ((uint32_t)(128 >> 4) << 24);
+}
+__device__ __forceinline__ uint64_t desc_sw128(uint32_t addr, uint32_t lbo, uint32_t sbo) {
+  return (uint64_t)((addr & 0x3ffff) >> 4) | (uint64_t)(lbo >> 4) << 16 | (uint64_t)(sbo >> 4) << 32 | (uint64_t)1 << 46 | (uint64_t)2 << 61;
+}
+__device__ __forceinline__ void mma_ts(uint32_t d_tmem, uint32_t a_tmem, uint64_t b_desc, uint32_t idesc, uint32_t accumulate) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "setp.ne.b32 p, %4, 0;\n\t"
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}"
+      ::"r"(d_tmem), "r"(a_tmem), "l"(b_desc), "r"(idesc), "r"(accumulate) : "memory");
+}
+__device__ __forceinline__ void tma4(void* dst, const CUtensorMap* map, int c0, int c1, int c2, int c3, uint64_t* bar) {
+  asm volatile("cp.async.bulk.tensor.4d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5}], [%6];"
+               ::"r"(smem_u32(dst)), "l"(map), "r"(c0), "r"(c1), "r"(c2), "r"(c3), "r"(smem_u32(bar)) : "memory");
+}
+__device__ __forceinline__ void ld32(uint32_t taddr, uint32_t* r) {   // completed by ld_wait
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15,"
+      " %16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
+      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]),
+        "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]),
+        "=r"(r[16]), "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]),
+        "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
+      : "r"(taddr) : "memory");
+}
+template <int N> __device__ __forceinline__ void ld_wait(uint32_t* r) {
+  asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+#pragma unroll
+  for (int i = 0; i < N; ++i) asm volatile("" : "+r"(r[i]));   // (the wait is tied to the registers it guards)
+}
+__device__ __forceinline__ void st32(uint32_t taddr, const uint32_t* v) {   // completed by st_wait
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16,"
+      " %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31, %32};"
+      ::"r"(taddr), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]),
+        "r"(v[8]), "r"(v[9]), "r"(v[10]), "r"(v[11]), "r"(v[12]), "r"(v[13]), "r"(v[14]), "r"(v[15]),
+        "r"(v[16]), "r"(v[17]), "r"(v[18]), "r"(v[19]), "r"(v[20]), "r"(v[21]), "r"(v[22]), "r"(v[23]),
+        "r"(v[24]), "r"(v[25]), "r"(v[26]), "r"(v[27]), "r"(v[28]), "r"(v[29]), "r"(v[30]), "r"(v[31]) : "memory");
+}
+__device__ __forceinline__ void st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+__device__ __forceinline__ float2 add2(float2 a, float2 b) {
+  float2 r;
+  asm("{.reg .b64 x, y, z; mov.b64 x, {%2, %3}; mov.b64 y, {%4, %5}; add.rn.f32x2 z, x, y; mov.b64 {%0, %1}, z;}" : "=f"(r.x), "=f"(r.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+  return r;
+}
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
+  float2 r;
+  asm("{.reg .b64 x, y, z, w; mov.b64 x, {%2, %3}; mov.b64 y, {%4, %5}; mov.b64 z, {%6, %7}; fma.rn.f32x2 w, x, y, z; mov.b64 {%0, %1}, w;}"
+      : "=f"(r.x), "=f"(r.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(c.x), "f"(c.y));
+  return r;
+}
+__device__ __forceinline__ float ex2a(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+
+// A unit: 256 queries of a request that share a key head.  Tile t has queries qb * 256 + 128 t ..; it sees its first `n_t` chunks.
+struct Unit { int req, first, n, len, qb, h, nch[2], all, c; };   // all: chunks of the unit (1 where nothing is seen), c: the next one
+
+__device__ __forceinline__ int tile_chunks(int n, int len, int q0, int group) {
+  const int nq = min(n * group - q0, 128);
+  if (nq <= 0) return 0;
+  const int last = len - n + (q0 + nq - 1) / group;
+  return last < 0 ? 0 : last / AT_CH + 1;
+}
+__device__ __forceinline__ void unit_sizes(Unit& u, int group) {
+  u.nch[0] = tile_chunks(u.n, u.len, u.qb * AT_ROWS, group);
+  u.nch[1] = tile_chunks(u.n, u.len, u.qb * AT_ROWS + 128, group);
+  u.all = max(1, max(u.nch[0], u.nch[1]));
+}
+__device__ __forceinline__ void unit_load(Unit& u, const AttendParams& P, int req) {
+  const Span s = request_span(P, req);
+  u.req = req; u.first = s.first; u.n = s.n; u.len = s.len;
+}
+__device__ __forceinline__ int blocks_of(int n, int group) { return (int)(((long long)n * group + AT_ROWS - 1) / AT_ROWS); }
+
+template <int HD> constexpr int at_smem() { return 1024 + AT_ROWS * HD * 2 + AT_STAGES * 2 * AT_CH * HD * 2 + 512; }
+
+// A CTA's walk over its part of the list; every role keeps one.
+struct Walk {
+  Unit u;
+  long long left;
+  int seg;
+  // the next part: chunks [c0, c1) of unit u; false at the end
+  __device__ __forceinline__ bool begin(int& c0, int& c1) const {
+    if (left <= 0) return false;
+    c0 = u.c;
+    c1 = (int)min((long long)u.all, c0 + left);
+    return true;
+  }
+  __device__ __forceinline__ void end(const AttendParams& P, int group, int c0, int c1) {
+    left -= c1 - c0;
+    ++seg;
+    if (left <= 0) return;
+    u.c = 0;                                        // (a part that ends inside a unit is the CTA's last one)
+    if (++u.h == P.kv_heads) {
+      u.h = 0;
+      if (++u.qb == blocks_of(u.n, group)) {
+        u.qb = 0;
+        int r = u.req;
+        do { unit_load(u, P, ++r); } while (u.n == 0);   // (there are steps left, so there is such a request)
+      }
+      unit_sizes(u, group);
+    }
+  }
+};
+
+template <typename T, int HD>
+__global__ void __launch_bounds__(AT_THREADS, 1) k_attend_tc(const __grid_constant__ TcParams J) {
+  constexpr bool BF = std::is_same<T, bf16>::value;
+  constexpr int HALVES = HD / 64, KBYTES = AT_CH * HD * 2, QTILE = 128 * HD * 2, NST = AT_STAGES;
+  extern __shared__ __align__(1024) uint8_t at_raw[];
+  const AttendParams& P = J.a;
+  uint8_t* qs = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(at_raw) + 1023) & ~(uintptr_t)1023);   // 2 tiles x HALVES x [128][128 bytes]
+  uint8_t* kst = qs + 2 * QTILE;                    // stages of K, then of V: HALVES x [128][128 bytes]
+  uint8_t* vst = kst + NST * KBYTES;
+  uint64_t* k_full = reinterpret_cast<uint64_t*>(vst + NST * KBYTES);
+  uint64_t* k_empty = k_full + NST; uint64_t* v_full = k_empty + NST; uint64_t* v_empty = v_full + NST;
+  uint64_t* v_fixed = v_empty + NST;                // the stage's edge chunk has been cleaned
+  uint64_t* q_full = v_fixed + NST; uint64_t* q_empty = q_full + 1;
+  uint64_t* s_full = q_empty + 1;                   // [2 tiles]
+  uint64_t* p_full = s_full + 2; uint64_t* o_full = p_full + 2; uint64_t* o_free = o_full + 2;
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(o_free + 2);
+  volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
+  volatile unsigned* valid_ring = reinterpret_cast<volatile unsigned*>(tmem_slot + 4);   // [4] page slices of a chunk that exist
+  volatile int* odd_ring = reinterpret_cast<volatile int*>(valid_ring + AT_RING);        // [4][2 warps] parts whose values had infinities or NaN taken out
+  __shared__ long long w_sum[AT_THREADS / 32];
+  __shared__ Walk s_walk;
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const int group = P.heads / P.kv_heads;
+  launch_dependents();
+  wait_prerequisites();
+  if (tid == 0) {
+    for (int s = 0; s < NST; ++s) { mbar_init(k_full + s, 1); mbar_init(k_empty + s, 1); mbar_init(v_full + s, 1); mbar_init(v_empty + s, 1); mbar_init(v_fixed + s, 2); }
+    mbar_init(q_full, 2); mbar_init(q_empty, 1);
+    for (int t = 0; t < 2; ++t) { mbar_init(s_full + t, 1); mbar_init(p_full + t, 4); mbar_init(o_full + t, 1); mbar_init(o_free + t, 4); }
+    *abort_flag = 0;
+    for (int i = 0; i < 2 * AT_RING; ++i) odd_ring[i] = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  // this CTA's part of the list
+  auto steps_of = [&](int i) -> long long {
+    Unit u;
+    unit_load(u, P, i);
+    long long n = 0;
+    const int blocks = blocks_of(u.n, group);
+    for (u.qb = 0; u.qb < blocks; ++u.qb) { unit_sizes(u, group); n += u.all; }
+    return n * P.kv_heads;
+  };
+  auto scan = [&](long long v, long long& all) {
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const long long x = __shfl_up_sync(0xffffffffu, v, o);
+      if (lane >= o) v += x;
+    }
+    __syncthreads();
+    if (lane == 31) w_sum[warp] = v;
+    __syncthreads();
+    long long before = 0;
+    all = 0;
+#pragma unroll
+    for (int w = 0; w < AT_THREADS / 32; ++w) { if (w < warp) before += w_sum[w]; all += w_sum[w]; }
+    return v + before;
+  };
+  long long total = 0;
+  for (int base = 0; base < P.n_req; base += AT_THREADS) {
+    long long all;
+    scan(base + tid < P.n_req ? steps_of(base + tid) : 0, all);
+    total += all;
+  }
+  const long long ctas = min((long long)gridDim.x, total);
+  Meta* meta = reinterpret_cast<Meta*>(P.ws) + blockIdx.x;
+  if (blockIdx.x >= ctas) {
+    if (tid == 0) *meta = Meta{};
+    return;
+  }
+  const long long x0 = total * blockIdx.x / ctas, x1 = total * (blockIdx.x + 1) / ctas;
+  {
+    long long before = 0;
+    for (int base = 0; base < P.n_req; base += AT_THREADS) {
+      const long long v = base + tid < P.n_req ? steps_of(base + tid) : 0;
+      long long all;
+      const long long incl = scan(v, all) + before;
+      if (x0 >= incl - v && x0 < incl) {
+        Walk w;
+        long long rem = x0 - (incl - v);
+        unit_load(w.u, P, base + tid);
+        for (w.u.qb = 0;; ++w.u.qb) {
+          unit_sizes(w.u, group);
+          if (rem < (long long)w.u.all * P.kv_heads) break;
+          rem -= (long long)w.u.all * P.kv_heads;
+        }
+        w.u.h = (int)(rem / w.u.all); w.u.c = (int)(rem - (long long)w.u.h * w.u.all);
+        w.left = x1 - x0; w.seg = 0;
+        s_walk = w;
+      }
+      before += all;
+    }
+  }
+  if (warp == 9) tmem_alloc(tmem_slot, 512);
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = *tmem_slot;
+  Walk W = s_walk;
+  int c0, c1;
+  int fills = 0;                                    // chunks copied (what is in flight is waited for after an abort)
+  // where a part's chunks reach past some query's last position
+  auto first_edge = [&](const Unit& u) { return max(0, (u.len - u.n + u.qb * AT_ROWS / group + 1)) / AT_CH; };
+  auto seen_chunks = [](const Unit& u) { return max(u.nch[0], u.nch[1]); };
+
+  if (warp == 8) {
+    // ------------------------------------------------------------------ K/V copies
+    const int slices = AT_CH / J.box_rows, half = lane / slices, sl = lane - half * slices;
+    bool ok = true;
+    while (ok && W.begin(c0, c1)) {
+      const Unit& u = W.u;
+      if (seen_chunks(u)) {
+        const int* table = P.table + (size_t)u.req * P.max_blocks;
+        auto page_of = [&](int c) {
+          const int p = c * AT_CH + sl * J.box_rows;
+          return half < HALVES && p < u.len ? __ldg(table + p / P.page_tokens) : -1;
+        };
+        int page = page_of(c0);
+        for (int c = c0; c < c1 && ok; ++c) {
+          const int next = c + 1 < c1 ? page_of(c + 1) : -1;
+          const bool is = page >= 0 && page < P.n_pages;
+          const unsigned valid = __ballot_sync(0xffffffffu, is || half > 0 || c * AT_CH + sl * J.box_rows >= u.len);
+          const int token = (c * AT_CH + sl * J.box_rows) % P.page_tokens, pg = is ? page : P.n_pages;
+          const int s = fills % NST, par = ((fills / NST) & 1) ^ 1;
+          for (int v = 0; v < 2 && ok; ++v) {
+            uint64_t* full = (v ? v_full : k_full) + s;
+            ok = __all_sync(0xffffffffu, mbar_wait((v ? v_empty : k_empty) + s, par, abort_flag, AT_WAIT));
+            if (!ok) break;
+            if (lane == 0) { if (v == 0) valid_ring[fills % AT_RING] = valid; mbar_expect_tx(full, KBYTES); }
+            __syncwarp();
+            if (half < HALVES)
+              tma4((v ? vst : kst) + (size_t)s * KBYTES + half * (AT_CH * 128) + sl * J.box_rows * 128, v ? &J.vmap : &J.kmap, half * 64,
+                   J.heads_outer ? token : u.h, J.heads_outer ? u.h : token, pg, full);
+            if (v == 1) ++fills;
+          }
+          page = next;
+        }
+      }
+      W.end(P, group, c0, c1);
+    }
+  } else if (warp == 9) {
+    // ------------------------------------------------------------------ MMA issue
+    if (lane == 0) {
+      const uint32_t idesc_s = instr_desc<BF>(AT_CH, 0), idesc_o = instr_desc<BF>(HD, 1);
+      int it = 0, fix[2] = {0, 0}, pc[2] = {0, 0}, oc[2] = {0, 0};
+      bool ok = true;
+      auto scores = [&](int t, int i) {              // S of tile t with the chunk in stage i % NST
+        const uint32_t qb = smem_u32(qs) + t * QTILE, kb = smem_u32(kst) + (i % NST) * KBYTES;
+#pragma unroll
+        for (int h = 0; h < HALVES; ++h)
+#pragma unroll
+          for (int k = 0; k < 4; ++k)
+            umma_bf16(tmem + t * 128, desc_sw128(qb + h * (128 * 128) + k * 32, 16, 1024), desc_sw128(kb + h * (AT_CH * 128) + k * 32, 16, 1024), idesc_s, (h | k) ? 1u : 0u);
+        umma_commit(s_full + t);
+      };
+      while (ok && W.begin(c0, c1)) {
+        const Unit& u = W.u;
+        const int n[2] = {max(0, min(c1, u.nch[0]) - c0), max(0, min(c1, u.nch[1]) - c0)}, L = max(n[0], n[1]);
+        const int edge = first_edge(u) - c0;          // chunks from here on are cleaned first
+        ok = mbar_wait(q_full, W.seg & 1, abort_flag, AT_WAIT);
+        if (ok && L) {
+          ok = mbar_wait(k_full + it % NST, (it / NST) & 1, abort_flag, AT_WAIT);
+          tc_fence_after();
+          if (ok) {
+            if (n[0]) scores(0, it);
+            if (n[1]) scores(1, it);
+            umma_commit(k_empty + it % NST);
+          }
+        }
+        if (ok && L <= 1) umma_commit(q_empty);
+        for (int j = 0; j < L && ok; ++j) {
+          const int vs = (it + j) % NST;
+          if (j >= edge) { ok = mbar_wait(v_fixed + vs, fix[vs] & 1, abort_flag, AT_WAIT); ++fix[vs]; }
+          else ok = mbar_wait(v_full + vs, ((it + j) / NST) & 1, abort_flag, AT_WAIT);
+          if (ok && j + 1 < L) ok = mbar_wait(k_full + (it + j + 1) % NST, ((it + j + 1) / NST) & 1, abort_flag, AT_WAIT);
+          const uint32_t vb = smem_u32(vst) + vs * KBYTES;
+#pragma unroll
+          for (int t = 0; t < 2; ++t) {
+            if (!ok || j >= n[t]) continue;
+            ok = mbar_wait(p_full + t, pc[t] & 1, abort_flag, AT_WAIT);
+            ++pc[t];
+            if (ok && j == 0) { ok = mbar_wait(o_free + t, (oc[t] & 1) ^ 1, abort_flag, AT_WAIT); ++oc[t]; }   // (the last part's O has been read)
+            if (!ok) continue;
+            tc_fence_after();
+#pragma unroll
+            for (int k = 0; k < AT_CH / 16; ++k)
+              mma_ts(tmem + 256 + t * 128, tmem + t * 128 + k * 8, desc_sw128(vb + k * 2048, AT_CH * 128, 1024), idesc_o, (j > 0 || k > 0) ? 1u : 0u);
+            if (j + 1 < n[t]) scores(t, it + j + 1);
+            else umma_commit(o_full + t);
+          }
+          if (!ok) break;
+          umma_commit(v_empty + vs);
+          if (j + 1 < L) umma_commit(k_empty + (it + j + 1) % NST);
+          if (j + 2 == L) umma_commit(q_empty);
+        }
+        it += L;
+        W.end(P, group, c0, c1);
+      }
+    }
+    __syncwarp();
+  } else if (warp >= 10) {
+    // ------------------------------------------------------------------ queries, and values of chunks at the edge
+    const int ft = tid - 320, pieces = P.hd / 8;
+    int it = 0;
+    bool ok = true;
+    while (ok && W.begin(c0, c1)) {
+      const Unit& u = W.u;
+      ok = __all_sync(0xffffffffu, mbar_wait(q_empty, (W.seg & 1) ^ 1, abort_flag, AT_WAIT));
+      if (!ok) break;
+      constexpr int PC = HD / 8;
+      for (int i = ft; i < AT_ROWS * PC; i += 64) {
+        const int r = i / PC, c = i % PC, qi = u.qb * AT_ROWS + r, j = qi / group;
+        const bool on = j < u.n && c < pieces;
+        const T* src = reinterpret_cast<const T*>(P.q) + (on ? (u.first + j) * P.q_row + (u.h * group + qi - j * group) * P.q_head + c * 8 : 0);
+        const uint32_t dst = smem_u32(qs) + (r >> 7) * QTILE + (c >> 3) * (128 * 128) + (r & 127) * 128 + (((c & 7) ^ (r & 7)) << 4);
+        asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(on ? 16 : 0) : "memory");
+      }
+      asm volatile("cp.async.commit_group;\n\tcp.async.wait_group 0;" ::: "memory");
+      asm volatile("fence.proxy.async.shared::cta;" ::: "memory");   // the tensor core reads these tiles through the async proxy
+      __syncwarp();
+      if (lane == 0) mbar_arrive(q_full);
+      const int L = max(max(0, min(c1, u.nch[0]) - c0), min(c1, u.nch[1]) - c0), edge = first_edge(u) - c0;
+      volatile int* odd_flag = odd_ring + W.seg % AT_RING * 2 + warp - 10;
+      if (lane == 0) *odd_flag = 0;
+      __syncwarp();
+      for (int j = max(edge, 0); j < L && ok; ++j) {
+        const int s = (it + j) % NST;
+        ok = __all_sync(0xffffffffu, mbar_wait(v_full + s, ((it + j) / NST) & 1, abort_flag, AT_WAIT));
+        if (!ok) break;
+        constexpr uint32_t EXPO = BF ? 0x7f80u : 0x7c00u;
+        const int left = u.len - (c0 + j) * AT_CH;   // positions of the chunk that the request has
+        bool odd = false;
+        for (int i = ft; i < AT_CH * PC; i += 64) {
+          const int r = i / PC, c = i % PC;
+          uint4* at = reinterpret_cast<uint4*>(vst + (size_t)s * KBYTES + (c >> 3) * (AT_CH * 128) + r * 128 + (((c & 7) ^ (r & 7)) << 4));
+          if (r >= left) { *at = make_uint4(0u, 0u, 0u, 0u); continue; }
+          uint4 w = *at;
+          uint32_t* e = reinterpret_cast<uint32_t*>(&w);
+          bool hit = false;
+#pragma unroll
+          for (int x = 0; x < 4; ++x) {
+            const uint32_t keep = ((e[x] & EXPO) == EXPO ? 0u : 0xffffu) | (((e[x] >> 16) & EXPO) == EXPO ? 0u : 0xffff0000u);
+            hit = hit || keep != 0xffffffffu;
+            e[x] &= keep;
+          }
+          if (hit) { *at = w; odd = true; }
+        }
+        if (odd) *odd_flag = 1;
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+        __syncwarp();
+        if (lane == 0) mbar_arrive(v_fixed + s);
+      }
+      it += L;
+      W.end(P, group, c0, c1);
+    }
+  } else {
+    // ------------------------------------------------------------------ softmax: one thread per query
+    const int t = warp >> 2, quad = warp & 3, ql = quad * 32 + lane;
+    const uint32_t sel = (uint32_t)(quad * 32) << 16, ts = tmem + t * 128 + sel, to = tmem + 256 + t * 128 + sel;
+    const float sc = P.scale * 1.4426950408889634f;   // (> 0: maxima are taken of the unscaled scores)
+    int sn = 0, on = 0, it = 0;
+    bool ok = true;
+    auto wait = [&](uint64_t* bar, uint32_t parity) { return (bool)__all_sync(0xffffffffu, mbar_wait(bar, parity, abort_flag, AT_WAIT)); };
+    while (ok && W.begin(c0, c1)) {
+      const Unit& u = W.u;
+      const int n_t = max(0, min(c1, u.nch[t]) - c0), L = max(max(0, min(c1, u.nch[0]) - c0), min(c1, u.nch[1]) - c0);
+      const int qi = u.qb * AT_ROWS + t * 128 + ql, jr = qi / group;
+      const bool mine = jr < u.n;
+      const int last = mine ? u.len - u.n + jr : -1;                                             // last position that this query sees
+      const int warp_first = u.len - u.n + (u.qb * AT_ROWS + t * 128 + quad * 32) / group;
+      float m_run = -INFINITY, l_run = 0.f;
+      for (int j = 0; j < n_t && ok; ++j) {
+        ok = wait(s_full + t, sn & 1);
+        ++sn;
+        if (!ok) break;
+        tc_fence_after();
+        uint32_t sr[AT_CH];
+#pragma unroll
+        for (int x = 0; x < AT_CH; x += 32) ld32(ts + x, sr + x);
+        ld_wait<AT_CH>(sr);
+        const int p0 = (c0 + j) * AT_CH;
+        const unsigned valid = valid_ring[(it + j) % AT_RING];
+        if (p0 + AT_CH - 1 > warp_first || valid != 0xffffffffu) {
+          const int shift = 31 - __clz(J.box_rows);
+#pragma unroll
+          for (int x = 0; x < AT_CH; ++x) if (p0 + x > last || !((valid >> (x >> shift)) & 1u)) sr[x] = 0xff800000u;   // -inf
+        }
+        float mx[4];
+#pragma unroll
+        for (int x = 0; x < 4; ++x) mx[x] = fmaxf(__uint_as_float(sr[x]), __uint_as_float(sr[x + 4]));
+#pragma unroll
+        for (int x = 8; x < AT_CH; x += 8)
+#pragma unroll
+          for (int y = 0; y < 4; ++y) mx[y] = fmaxf(fmaxf(mx[y], __uint_as_float(sr[x + y])), __uint_as_float(sr[x + y + 4]));
+        const float seen = fmaxf(m_run, fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * sc);
+        // The reference follows the running maximum only when that has moved by more than 2^8: weights of up to 256 are as exact, and
+        // O is rescaled a few times a row instead of every chunk.
+        const float m_new = (seen > m_run + 8.0f || m_run == -INFINITY) ? seen : m_run;
+        const float off = m_new == -INFINITY ? 0.f : m_new;
+        const float corr = ex2a(m_run - off);
+        const float2 s2 = make_float2(sc, sc), o2 = make_float2(-off, -off);
+        float2 sum[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
+        if (j > 0 && __any_sync(0xffffffffu, corr != 1.0f)) {   // (the scores' completion is also that of the products before them)
+#pragma unroll 1
+          for (int d = 0; d < HD; d += 32) {
+            uint32_t v[32];
+            ld32(to + d, v);
+            ld_wait<32>(v);
+#pragma unroll
+            for (int x = 0; x < 32; ++x) v[x] = __float_as_uint(__uint_as_float(v[x]) * corr);
+            st32(to + d, v);
+          }
+        }
+#pragma unroll
+        for (int x = 0; x < AT_CH; x += 2) {
+          float2 e = fma2(make_float2(__uint_as_float(sr[x]), __uint_as_float(sr[x + 1])), s2, o2);
+          e.x = ex2a(e.x); e.y = ex2a(e.y);
+          sum[(x >> 1) & 1] = add2(sum[(x >> 1) & 1], e);
+          sr[x / 2] = pack2<T>(e.x, e.y);
+        }
+        st32(ts, sr);
+        st32(ts + 32, sr + 32);
+        sum[0] = add2(sum[0], sum[1]);
+        l_run = l_run * corr + (sum[0].x + sum[0].y);
+        m_run = m_new;
+        st_wait();
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(p_full + t);
+      }
+      if (!ok) break;
+      const bool cut = c0 > 0 || c1 < u.all;
+      float* part = reinterpret_cast<float*>(reinterpret_cast<unsigned char*>(P.ws) + (size_t)gridDim.x * sizeof(Meta)) +
+                    (size_t)(2 * blockIdx.x + (W.seg ? 1 : 0)) * (AT_ROWS * (P.hd + 2));
+      const int row = t * 128 + ql;
+      T* dst = reinterpret_cast<T*>(P.o) + (u.first + jr) * P.o_row + (u.h * group + qi - jr * group) * P.o_head;
+      const float inv = m_run == -INFINITY ? 0.f : 1.f / l_run;
+      if (n_t) {
+        ok = wait(o_full + t, on & 1);
+        ++on;
+        if (!ok) break;
+        tc_fence_after();
+      }
+      const bool odd = odd_ring[W.seg % AT_RING * 2] | odd_ring[W.seg % AT_RING * 2 + 1];
+#pragma unroll 1
+      for (int d = 0; d < HD; d += 32) {
+        uint32_t v[32];
+        __syncwarp();
+        if (n_t) { ld32(to + d, v); ld_wait<32>(v); }
+        else {
+#pragma unroll
+          for (int x = 0; x < 32; ++x) v[x] = 0u;
+        }
+        if (!mine) continue;
+        if (odd) {                                    // infinities and NaN that were taken out, of positions that this query sees
+          for (int p = max(first_edge(u), c0) * AT_CH; p <= min(last, c1 * AT_CH - 1); ++p) {
+            const int b = p / P.page_tokens, page = P.table[(size_t)u.req * P.max_blocks + b];
+            if (page < 0 || page >= P.n_pages) continue;
+            const T* vr = reinterpret_cast<const T*>(P.vc) + page * P.page_stride + (p - b * P.page_tokens) * P.token_stride + u.h * P.head_stride + d;
+#pragma unroll 1
+            for (int x = 0; x < 32 && d + x < P.hd; ++x) {
+              const float y = to_f32(vr[x]);
+              if (!isfinite(y)) {
+#pragma unroll
+                for (int z = 0; z < 32; ++z) if (z == x) v[z] = __float_as_uint(__uint_as_float(v[z]) + y);
+              }
+            }
+          }
+        }
+        if (cut) {
+#pragma unroll
+          for (int x = 0; x < 32; x += 4)
+            if (d + x < P.hd) *reinterpret_cast<uint4*>(part + (size_t)row * P.hd + d + x) = make_uint4(v[x], v[x + 1], v[x + 2], v[x + 3]);
+        } else {
+#pragma unroll
+          for (int x = 0; x < 32; x += 8)
+            if (d + x < P.hd) {
+              uint4 w;
+              w.x = pack2<T>(__uint_as_float(v[x]) * inv, __uint_as_float(v[x + 1]) * inv); w.y = pack2<T>(__uint_as_float(v[x + 2]) * inv, __uint_as_float(v[x + 3]) * inv);
+              w.z = pack2<T>(__uint_as_float(v[x + 4]) * inv, __uint_as_float(v[x + 5]) * inv); w.w = pack2<T>(__uint_as_float(v[x + 6]) * inv, __uint_as_float(v[x + 7]) * inv);
+              *reinterpret_cast<uint4*>(dst + d + x) = w;
+            }
+        }
+      }
+      if (cut && mine) { part[(size_t)AT_ROWS * P.hd + row] = m_run; part[(size_t)AT_ROWS * (P.hd + 1) + row] = l_run; }
+      if (n_t) {
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(o_free + t);
+      }
+      it += L;
+      W.end(P, group, c0, c1);
+    }
+  }
+  // ------------------------------------------------------------------ teardown
+  __syncwarp();
+  __syncthreads();
+  if (*abort_flag) {
+    if (warp == 8 && lane == 0) {
+      const long long t0 = clock64();
+      for (int f = max(0, fills - NST); f <= fills; ++f)      // (the last one may have been requested for K alone)
+        for (int v = 0; v < 2; ++v)
+          while (!mbar_try((v ? v_full : k_full) + f % NST, (f / NST) & 1))
+            if (clock64() - t0 > 2000000) break;
+      settle(t0);
+    }
+    __syncthreads();
+  }
+  if (tid == 0) {
+    // the unit that goes on in the next CTAs, if one begins here and does not end
+    Walk w = s_walk;
+    Meta m{};
+    m.failed = *abort_flag;
+    int a, b;
+    while (w.begin(a, b)) {
+      if (a == 0 && b < w.u.all) {
+        const long long end = x1 + (w.u.all - b);               // one past the unit's last step
+        long long e = (end * ctas - 1) / total;                 // the CTA whose part holds that step (about; corrected below)
+        while (e > 0 && total * e / ctas >= end) --e;
+        while (total * (e + 1) / ctas < end) ++e;
+        m.parts = (int)(e - blockIdx.x) + 1;
+        m.slot = 2 * blockIdx.x + (w.seg ? 1 : 0); m.first = w.u.first; m.n = w.u.n; m.qb = w.u.qb; m.h = w.u.h;
+      }
+      w.end(P, group, a, b);
+    }
+    *meta = m;
+  }
+  if (warp == 9) { tc_fence_after(); tmem_dealloc(tmem, 512); }
+}
+
+typedef CUresult (*EncodeFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*, const cuuint32_t*, const cuuint32_t*,
+                             CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+
+template <typename T, int HD> int launch(const TcParams& J, cudaStream_t st) {
+  auto kern = k_attend_tc<T, HD>;
+  SCK(cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, at_smem<HD>()));
+  kern<<<AM_SMS, AT_THREADS, at_smem<HD>(), st>>>(J);
+  SCK(cudaGetLastError());
+  return launch_join<T, AT_ROWS, true>(J.a, AM_SMS, 8, st);
+}
+
+}  // namespace
+
+// What the tensor maps and the page slices ask for; everything else goes the other way.
+bool tc_takes(const stairs_paged* c, float scale) {
+  const int p = c->page_tokens;
+  auto stride = [](int64_t s, int n) { return n == 1 || (s > 0 && s < (1ll << 39)); };
+  return c->head_dim <= 128 && (p % AT_CH == 0 || (p >= 8 && p < AT_CH && (p & (p - 1)) == 0)) && scale > 0.f && stride(c->token_stride, 2) &&
+         stride(c->head_stride, c->n_kv_heads) && stride(c->page_stride, c->n_pages);
+}
+
+size_t tc_workspace(int hd) { return (size_t)AM_SMS * (sizeof(Meta) + (size_t)2 * AT_ROWS * (hd + 2) * 4); }
+
+int launch_tc(const AttendParams& P, int dtype, cudaStream_t st) {
+  static EncodeFn encode = nullptr;              // (the driver's function: the same whoever looks it up)
+  if (!encode) {
+    void* fn = nullptr;
+    cudaDriverEntryPointQueryResult q;
+    SCK(cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &fn, cudaEnableDefault, &q));
+    if (!fn || q != cudaDriverEntryPointSuccess) return static_fail(STAIRS_ECUDA, "cuTensorMapEncodeTiled is not available from the driver");
+    encode = reinterpret_cast<EncodeFn>(fn);
+  }
+  TcParams J;
+  J.a = P;
+  J.box_rows = P.page_tokens < AT_CH ? P.page_tokens : AT_CH;
+  // the coordinates between the elements and the pages: the one of the smaller stride first
+  J.heads_outer = P.kv_heads > 1 && P.head_stride > P.token_stride;
+  const cuuint64_t tok = (cuuint64_t)P.token_stride * 2, head = (cuuint64_t)(P.kv_heads > 1 ? P.head_stride : P.token_stride) * 2;   // (one head: any stride)
+  const cuuint64_t dims[4] = {(cuuint64_t)P.hd, (cuuint64_t)(J.heads_outer ? P.page_tokens : P.kv_heads), (cuuint64_t)(J.heads_outer ? P.kv_heads : P.page_tokens), (cuuint64_t)P.n_pages};
+  const cuuint64_t strides[3] = {J.heads_outer ? tok : head, J.heads_outer ? head : tok, (cuuint64_t)(P.n_pages > 1 ? P.page_stride : P.token_stride) * 2};
+  const cuuint32_t box[4] = {64u, J.heads_outer ? (cuuint32_t)J.box_rows : 1u, J.heads_outer ? 1u : (cuuint32_t)J.box_rows, 1u}, es[4] = {1, 1, 1, 1};
+  for (int v = 0; v < 2; ++v)
+    if (encode(v ? &J.vmap : &J.kmap, dtype == DT_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 4, const_cast<void*>(v ? P.vc : P.kc), dims, strides, box,
+               es, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
+      return static_fail(STAIRS_ECUDA, "stairs_attend_static: cuTensorMapEncodeTiled failed for the cache");
+  if (P.hd <= 64) return dtype == DT_BF16 ? launch<bf16, 64>(J, st) : launch<__half, 64>(J, st);
+  return dtype == DT_BF16 ? launch<bf16, 128>(J, st) : launch<__half, 128>(J, st);
+}
+
+}  // namespace att
+}  // namespace stairs
