@@ -412,11 +412,16 @@ __global__ void __launch_bounds__(AT_THREADS, 1) k_attend_tc(const __grid_consta
       const bool mine = jr < u.n;
       const int last = mine ? u.len - u.n + jr : -1;                                             // last position that this query sees
       const int warp_first = u.len - u.n + (u.qb * AT_ROWS + t * 128 + quad * 32) / group;
+      const bool idle = u.qb * AT_ROWS + t * 128 + quad * 32 >= u.n * group;                     // no query in this warp: its rows hold anything
       float m_run = -INFINITY, l_run = 0.f;
       for (int j = 0; j < n_t && ok; ++j) {
         ok = wait(s_full + t, sn & 1);
         ++sn;
         if (!ok) break;
+        if (idle) {
+          if (lane == 0) mbar_arrive(p_full + t);
+          continue;
+        }
         tc_fence_after();
         uint32_t sr[AT_CH];
 #pragma unroll
@@ -487,7 +492,7 @@ __global__ void __launch_bounds__(AT_THREADS, 1) k_attend_tc(const __grid_consta
       }
       const bool odd = odd_ring[W.seg % AT_RING * 2] | odd_ring[W.seg % AT_RING * 2 + 1];
 #pragma unroll 1
-      for (int d = 0; d < HD; d += 32) {
+      for (int d = 0; d < HD && !idle; d += 32) {
         uint32_t v[32];
         __syncwarp();
         if (n_t) { ld32(to + d, v); ld_wait<32>(v); }

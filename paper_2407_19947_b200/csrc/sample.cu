@@ -19,12 +19,12 @@ typedef unsigned long long u64;
 struct SampleParams {
   const void* logits; const float* u; const int* draft; int* tokens; int* accept;
   long long ld;
-  int vocab, n_req, n_rows, k_max, bits;      // bits: the largest weight is 2^bits
+  int vocab, n_req, n_rows, k_max, bits, list;   // bits: the largest weight is 2^bits; list: entries of a row's list
   int off[STAIRS_SAMPLE_MAX_REQ], k[STAIRS_SAMPLE_MAX_REQ];
   stairs_sampling s[STAIRS_SAMPLE_MAX_REQ];
 };
 
-constexpr int NB = 2048, SMALL = 256;        // bins of a histogram; most elements of a bin that are ranked one against another
+constexpr int NB = 1024, SMALL = 256;        // bins of a histogram; most elements of a bin that are ranked one against another
 
 // (larger score, then lower index) as one number
 __device__ __forceinline__ uint32_t ordered(float x) {
@@ -77,82 +77,192 @@ template <int NT> struct BlockOps {
   }
 };
 
-template <typename T, int NT, bool STAGED>
-__global__ void __launch_bounds__(NT, STAGED && sizeof(T) == 4 ? 1 : 2) k_sample(const __grid_constant__ SampleParams P) {
+// What the CTAs of a row tell one another.
+struct Told { float m, bound, weight; int count, first, bin; u64 mass; };
+
+constexpr int SP_THREADS = 512, FINE = 8192;   // FINE: bins of a count of scores, in the list's place (which so has FINE / 2 entries at least)
+template <typename T> constexpr int sp_vec() { return 16 / sizeof(T); }
+// elements of a CTA's slice of the vocabulary, and its shared memory
+__host__ __device__ inline int sp_slice(int vocab, int cl) { return ((vocab + cl - 1) / cl + 63) / 64 * 64; }
+template <typename T> size_t sp_smem(int vocab, int cl, bool staged, int list) {
+  return (size_t)(NB + list + SMALL + 64) * 8 + (staged ? ((size_t)sp_slice(vocab, cl) + 2 * sp_vec<T>()) * sizeof(T) : 0);
+}
+
+// One row: CL CTAs (a cluster where there are several), each with a slice of the vocabulary in shared memory.
+//  1. The slice is loaded; every thread keeps the largest score that it saw.  These 512 numbers bound what can be kept: at least k scores are
+//     as large as the k-th of them, and scores of weight below (1 - top_p) / vocab of the weight that they have together are never in the
+//     first top_p of the whole (all such tokens together weigh less than the rest).
+//     Where that is not sharp - a top-p without a top-k, a top-k above 512 - scores above the bound are counted in 8192 bins, and the bound is
+//     the bin down to which a CTA holds its share of the count, or surely top_p of its own weight (each score taken for the smallest of its bin).
+//  2. One pass: scores above the bound are listed; rows that need it are weighed as a whole.
+//  3. The first CTA gets the lists and filters and draws among a few dozen (ranked one against another) to some thousand tokens (by
+//     histograms).  Rows without top-k and top-p need no list: the running sum is looked up by CTA, warp and thread.  Rows whose list
+//     would not fit (flat scores with a large top_p) are worked on as a whole by the first CTA, with histograms over all scores.
+template <typename T, int CL, bool STAGED>
+__global__ void __launch_bounds__(SP_THREADS, 2) k_sample(const __grid_constant__ SampleParams P) {
+  constexpr int NT = SP_THREADS, NW = NT / 32, VN = sp_vec<T>();
   extern __shared__ __align__(16) unsigned char sp_sm[];
   u64* hist = reinterpret_cast<u64*>(sp_sm);
   u64* list = hist + NB;
-  u64* list_w = list + SMALL;
-  double* tab = reinterpret_cast<double*>(list_w + SMALL);
+  u64* small_w = list + P.list;
+  double* tab = reinterpret_cast<double*>(small_w + SMALL);
   T* xs = reinterpret_cast<T*>(tab + 64);
-  __shared__ u64 red[NT / 32 + 1];
-  __shared__ u64 s_pick[4];
+  __shared__ u64 red[NW + 1], s_pick[4];
   __shared__ int s_int[4];
-  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, row = blockIdx.x, V = P.vocab;
-  constexpr int NW = NT / 32;
+  __shared__ Told told_all[3][CL];            // (a set for each time: a fast CTA may send its next numbers while a slow one still reads the last)
+  Told* told = told_all[0];
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, row = blockIdx.x / CL, rank = blockIdx.x % CL, V = P.vocab;
   launch_dependents();
+  if (CL > 1) asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");
   wait_prerequisites();
-  if (tid < 64) tab[tid] = exp2((double)P.bits + tid / 64.0);
-  int lo = 0, hi = P.n_req - 1;
-  while (lo < hi) {
-    const int mid = (lo + hi + 1) >> 1;
-    if (P.off[mid] <= row) lo = mid; else hi = mid - 1;
+  int lo_r = 0, hi_r = P.n_req - 1;
+  while (lo_r < hi_r) {
+    const int mid = (lo_r + hi_r + 1) >> 1;
+    if (P.off[mid] <= row) lo_r = mid; else hi_r = mid - 1;
   }
-  const int req = lo, r_in = row - P.off[req];
+  const int req = lo_r, r_in = row - P.off[req];
   const stairs_sampling S = P.s[req];
   const T* logits = reinterpret_cast<const T*>(P.logits) + (size_t)row * P.ld;
-  auto clean = [](float x) { return x == x ? x + 0.f : -INFINITY; };   // (-0 counts as 0)
-  auto get = [&](int i) { return clean(to_f32(STAGED ? xs[i] : logits[i])); };
+  const int slice = sp_slice(V, CL), lo = min(rank * slice, V), n = min(slice, V - lo);
+  if (tid < 64) tab[tid] = exp2((double)P.bits + tid / 64.0);
+  auto clean = [](float x) { return x == x ? x + 0.f : -INFINITY; };   // (NaN counts as -infinity, -0 as 0)
 
-  // the row's extent: largest and smallest score above -infinity
-  float mx = -INFINITY, mn = INFINITY;
+  // The slice in whole vectors from the first 16-byte boundary at or before it; what is outside of it reads as -infinity.
+  const int sh = (int)((reinterpret_cast<uintptr_t>(logits + lo) & 15) / sizeof(T)), vecs = n > 0 ? (sh + n + VN - 1) / VN : 0;
+  const T* base = logits + lo - sh;
+  auto load = [&](int v, T* e) {                    // vector v, from memory
+    if (v * VN >= sh && (v + 1) * VN <= sh + n) *reinterpret_cast<uint4*>(e) = __ldg(reinterpret_cast<const uint4*>(base) + v);
+    else {
+#pragma unroll
+      for (int c = 0; c < VN; ++c) { const int i = v * VN + c; e[c] = i >= sh && i < sh + n ? base[i] : from_f32<T>(-INFINITY); }
+    }
+  };
+  auto vec = [&](int v, float* x) {                 // the same, cleaned, for the passes behind the first
+    alignas(16) T e[VN];
+    if (STAGED) *reinterpret_cast<uint4*>(e) = *(reinterpret_cast<const uint4*>(xs) + v); else load(v, e);
+#pragma unroll
+    for (int c = 0; c < VN; ++c) x[c] = clean(to_f32(e[c]));
+  };
+  float tmax = -INFINITY;
   {
-    constexpr int VN = 16 / sizeof(T);
-    const int head = min(V, (int)(((16 - (reinterpret_cast<uintptr_t>(logits) & 15)) & 15) / sizeof(T)));   // elements before the first whole vector
-    const int vecs = (V - head) / VN;
-    auto look = [&](T raw, int i) {
-      if (STAGED) xs[i] = raw;
-      const float x = clean(to_f32(raw));
-      mx = fmaxf(mx, x);
-      mn = fminf(mn, x == -INFINITY ? INFINITY : x);
-    };
     constexpr int UN = 4;
     for (int v0 = tid; v0 < vecs; v0 += NT * UN) {
-      uint4 q[UN];
+      alignas(16) T e[UN][VN];
 #pragma unroll
-      for (int j = 0; j < UN; ++j) if (v0 + j * NT < vecs) q[j] = __ldg(reinterpret_cast<const uint4*>(logits + head) + v0 + j * NT);
+      for (int j = 0; j < UN; ++j) if (v0 + j * NT < vecs) load(v0 + j * NT, e[j]);
 #pragma unroll
       for (int j = 0; j < UN; ++j)
         if (v0 + j * NT < vecs) {
-          const T* e = reinterpret_cast<const T*>(&q[j]);
+          if (STAGED) *(reinterpret_cast<uint4*>(xs) + v0 + j * NT) = *reinterpret_cast<uint4*>(e[j]);
 #pragma unroll
-          for (int c = 0; c < VN; ++c) look(e[c], head + (v0 + j * NT) * VN + c);
+          for (int c = 0; c < VN; ++c) tmax = fmaxf(tmax, to_f32(e[j][c]));   // (NaN is passed over)
         }
     }
-    for (int i = tid; i < head; i += NT) look(logits[i], i);
-    for (int i = head + vecs * VN + tid; i < V; i += NT) look(logits[i], i);
+    tmax += 0.f;
   }
-  {
+  auto extremes = [&](float& mx, float& mn) {       // over the block: largest mx, smallest mn
     const uint32_t a = __reduce_max_sync(0xffffffffu, ordered(mx)), b = __reduce_min_sync(0xffffffffu, ordered(mn));
+    __syncthreads();
     if (lane == 0) red[warp] = ((u64)a << 32) | b;
     __syncthreads();
     uint32_t A = 0u, B = 0xffffffffu;
 #pragma unroll
     for (int w = 0; w < NW; ++w) { A = max(A, (uint32_t)(red[w] >> 32)); B = min(B, (uint32_t)red[w]); }
     mx = unordered(A); mn = unordered(B);
-    __syncthreads();
+  };
+  auto tell = [&](const Told& t) {                  // this CTA's numbers to all; then `told` is complete
+    if (CL == 1) {
+      if (tid == 0) told[0] = t;
+      __syncthreads();
+    } else {
+      if (tid < CL) {
+        uint32_t at;
+        asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"(smem_addr(told + rank)), "r"(tid));
+        const uint32_t* w = reinterpret_cast<const uint32_t*>(&t);
+#pragma unroll
+        for (int i = 0; i < (int)sizeof(Told) / 4; ++i) asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(at + 4 * i), "r"(w[i]) : "memory");
+      }
+      asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+    }
+  };
+  if (CL > 1) asm volatile("barrier.cluster.wait.aligned;" ::: "memory");   // every CTA of the cluster runs
+
+  const bool use_k = S.top_k > 0 && S.top_k < V, use_p = S.top_p < 1.f;
+  Told mine{};
+  float mn = tmax == -INFINITY ? INFINITY : tmax;
+  mine.m = tmax;
+  extremes(mine.m, mn);
+  mine.bound = -INFINITY;
+  if (S.temperature > 0.f && mine.m > -INFINITY) {
+    if (use_k && S.top_k <= NT) {
+      // the k-th largest of the threads' maxima, or one a little smaller: a histogram of them
+      const int have = __syncthreads_count(tmax > -INFINITY);
+      if (have >= S.top_k) {
+        const float range = mine.m - mn;
+        mine.bound = mn;
+        if (range > 1e-30f && range < INFINITY) {
+          const float scale = (float)NB / range;
+          for (int b = tid; b < NB; b += NT) hist[b] = 0;
+          __syncthreads();
+          const int bin = tmax > -INFINITY ? min(NB - 1, (int)((mine.m - tmax) * scale)) : NB;
+          if (bin < NB) atomicAdd(reinterpret_cast<unsigned*>(hist + bin), 1u);
+          __syncthreads();
+          u64 c[NB / NT], sum = 0, all;
+#pragma unroll
+          for (int j = 0; j < NB / NT; ++j) { c[j] = hist[tid * (NB / NT) + j]; sum += c[j]; }
+          u64 before = BlockOps<NT>::scan(sum, red, all) - sum;
+#pragma unroll
+          for (int j = 0; j < NB / NT; ++j) {
+            if (before < (u64)S.top_k && before + c[j] >= (u64)S.top_k) s_int[0] = tid * (NB / NT) + j;
+            before += c[j];
+          }
+          __syncthreads();
+          float a = -INFINITY, b = bin <= s_int[0] ? tmax : INFINITY;
+          extremes(a, b);
+          mine.bound = b;
+        }
+      }
+    } else if (use_p && !use_k) {
+      float w = tmax == mine.m ? 1.f : __expf((tmax - mine.m) / S.temperature);
+      w = warp_sum(w);
+      __syncthreads();
+      if (lane == 0) red[warp] = __float_as_uint(w);
+      __syncthreads();
+      float sum = 0.f;
+#pragma unroll
+      for (int i = 0; i < NW; ++i) sum += __uint_as_float((uint32_t)red[i]);
+      mine.weight = sum;
+    }
   }
+  tell(mine);
+  float mx = -INFINITY, bound = -INFINITY;
+#pragma unroll
+  for (int c = 0; c < CL; ++c) { mx = fmaxf(mx, told[c].m); bound = fmaxf(bound, told[c].bound); }
   int token = -1;
+  bool writer = rank == 0;
   if (mx == -INFINITY) {
     // nothing to draw
   } else if (S.temperature == 0.f) {
     int best = 0x7fffffff;
-    for (int i = tid; i < V; i += NT) if (get(i) == mx) { best = i; break; }
+    if (mine.m == mx)
+      for (int v = tid; v < vecs; v += NT) {
+        float x[VN];
+        vec(v, x);
+#pragma unroll
+        for (int c = VN - 1; c >= 0; --c) if (x[c] == mx) best = min(best, lo + v * VN + c - sh);
+        if (best < 0x7fffffff) break;
+      }
     best = __reduce_min_sync(0xffffffffu, best);
+    __syncthreads();
     if (lane == 0) red[warp] = (u64)best;
     __syncthreads();
 #pragma unroll
     for (int w = 0; w < NW; ++w) best = min(best, (int)red[w]);
+    mine.first = best;
+    told = told_all[1];
+    tell(mine);
+#pragma unroll
+    for (int c = 0; c < CL; ++c) best = min(best, told[c].first);
     token = best;
   } else {
     Weigher W;
@@ -161,159 +271,377 @@ __global__ void __launch_bounds__(NT, STAGED && sizeof(T) == 4 ? 1 : 2) k_sample
     // what may weigh anything: scores not much further than this below the largest
     const float nats = S.min_p > 0.f ? fminf(-logf(S.min_p) + 1e-3f, (P.bits + 1.5f) * 0.6931472f) : (P.bits + 1.5f) * 0.6931472f;
     W.cut = nats * S.temperature * 1.00001f;
-    u64 thr = 0;                               // kept: keys from here up
-    const int seg = ((V + NW - 1) / NW + 31) / 32 * 32;
-
-    // Lowers the list of kept keys to the first ones whose count (mass: weight) reaches a bound: a histogram of the scores, its bin where the bound is
-    // passed, then that bin's elements, finer again while they are many.
-    auto find = [&](const bool mass) {
-      const float range = fminf(mx - mn, W.cut), fscale = range > 1e-30f ? (float)NB / range : 0.f;
-      uint32_t kmin = 0u, kmax = 0xffffffffu;   // ordered scores of the current interval
-      int shift = -1;                           // < 0: bins are linear in the score
-      if (fscale == 0.f) { kmin = ordered(mn); kmax = ordered(mx); shift = max(0, 32 - __clz(kmax - kmin) - 11); }
-      u64 base = 0;
-      double target = (double)S.top_k;
-      for (bool top = true;; top = false) {
-        auto bin_of = [&](float x, uint32_t o) { return shift < 0 ? (x == mx ? 0 : min(NB - 1, (int)((mx - x) * fscale))) : (int)((kmax - o) >> shift); };
-        for (int b = tid; b < NB; b += NT) hist[b] = 0;
-        __syncthreads();
-        for (int i0 = warp * seg; i0 < min(V, (warp + 1) * seg); i0 += 32) {
-          const int i = i0 + lane;
-          const float x = i < V ? get(i) : -INFINITY;
-          const uint32_t o = ordered(x);
-          if (x > -INFINITY && W.eligible(x) && o >= kmin && o <= kmax && full_key(o, i) >= thr) {
-            const u64 w = mass ? W(x) : 1;
-            if (w) atomicAdd(hist + bin_of(x, o), w);
-          }
-        }
-        __syncthreads();
-        u64 mine[NB / NT], sum = 0, total;
+    const float uf = P.u[row];
+    const float u = uf >= 0.f ? fminf(uf, 0.99999994f) : 0.f;   // (NaN: 0)
+    bool whole = false;                        // the first CTA works on the whole row
+    const bool by_mass = use_p && !use_k;
+    if (by_mass) {
+      float sum = 0.f;
 #pragma unroll
-        for (int j = 0; j < NB / NT; ++j) { mine[j] = hist[tid * (NB / NT) + j]; sum += mine[j]; }
-        u64 incl = BlockOps<NT>::scan(sum, red, total);
-        if (top && mass) target = (double)S.top_p * (double)total;
-        if (top && !mass && (double)total <= target) return;   // no more than that: all stay
-        u64 c = incl - sum;
+      for (int c = 0; c < CL; ++c) sum += told[c].m == -INFINITY ? 0.f : told[c].weight * (told[c].m == mx ? 1.f : __expf((told[c].m - mx) / S.temperature));
+      const float least = (1.f - S.top_p) * sum * 0.999f / (float)V, d = -logf(least) * S.temperature * 1.0001f;
+      bound = mx - d - 1e-6f * (fabsf(mx) + d);
+      if (!(bound > -INFINITY)) bound = -INFINITY;
+    }
+    const int wv = (vecs + NW - 1) / NW, v_end = min(vecs, (warp + 1) * wv);   // a warp's vectors lie together: sums in the order of the indices
+    const bool listed = use_k || use_p;
+    // each_vec(f): f(v, x, on) for this warp's vectors, 32 at a time (on: it exists)
+    auto each_vec = [&](auto&& f) {
+      for (int v0 = warp * wv; v0 < v_end; v0 += 32) {
+        const int v = v0 + lane;
+        float x[VN];
+        if (v < v_end) vec(v, x);
+        else {
 #pragma unroll
-        for (int j = 0; j < NB / NT; ++j) {
-          if ((double)(base + c) < target && !((double)(base + c + mine[j]) < target)) { s_int[0] = tid * (NB / NT) + j; s_pick[0] = c; }
-          c += mine[j];
+          for (int c = 0; c < VN; ++c) x[c] = -INFINITY;
         }
-        if (tid == 0) { s_int[1] = 0; s_int[2] = -1; s_int[3] = 0; }   // elements of the bin; smallest and largest score (as unsigned)
-        __syncthreads();
-        const int bin = s_int[0];
-        base += s_pick[0];
-        uint32_t omin = 0xffffffffu, omax = 0u;
-        for (int i0 = warp * seg; i0 < min(V, (warp + 1) * seg); i0 += 32) {
-          const int i = i0 + lane;
-          const float x = i < V ? get(i) : -INFINITY;
-          const uint32_t o = ordered(x);
-          if (x > -INFINITY && W.eligible(x) && o >= kmin && o <= kmax && full_key(o, i) >= thr && bin_of(x, o) == bin) {
-            const int at = atomicAdd(s_int + 1, 1);
-            if (at < SMALL) list[at] = full_key(o, i);
-            omin = min(omin, o); omax = max(omax, o);
-          }
-        }
-        omin = __reduce_min_sync(0xffffffffu, omin); omax = __reduce_max_sync(0xffffffffu, omax);
-        if (lane == 0 && omin <= omax) { atomicMin(reinterpret_cast<unsigned*>(s_int + 2), omin); atomicMax(reinterpret_cast<unsigned*>(s_int + 3), omax); }
-        __syncthreads();
-        const int n = s_int[1];
-        kmin = (uint32_t)s_int[2]; kmax = (uint32_t)s_int[3];
-        if (n <= SMALL) {
-          if (tid < n) list_w[tid] = mass ? W(unordered((uint32_t)(list[tid] >> 32))) : 1;
-          if (tid == 0) s_pick[1] = ~0ull;
-          __syncthreads();
-          if (tid < n) {
-            const u64 key = list[tid];
-            u64 above = 0;
-            for (int j = 0; j < n; ++j) above += list[j] > key ? list_w[j] : 0;
-            if ((double)(base + above) < target) atomicMin(s_pick + 1, key);
-          }
-          __syncthreads();
-          thr = s_pick[1];
-          __syncthreads();
-          return;
-        }
-        if (kmin == kmax) {
-          // equal scores: the first of them by index, as many as the bound needs
-          const u64 w = mass ? W(unordered(kmin)) : 1;
-          u64 keep = w ? (u64)((target - (double)base) / (double)w) : 0;
-          if (keep > 0) --keep;
-          while ((double)(base + keep * w) < target && keep < (u64)n) ++keep;   // (the division may be off by one)
-          if (keep == 0) keep = 1;
-          u64 cnt = 0;
-          for (int i0 = warp * seg; i0 < min(V, (warp + 1) * seg); i0 += 32) {
-            const int i = i0 + lane;
-            cnt += __popc(__ballot_sync(0xffffffffu, i < V && ordered(get(i)) == kmin));
-          }
-          __syncthreads();
-          if (lane == 0) red[warp] = cnt;
-          __syncthreads();
-          u64 before = 0;
-          for (int w2 = 0; w2 < warp; ++w2) before += red[w2];
-          if (before < keep && keep <= before + cnt)
-            for (int i0 = warp * seg; i0 < min(V, (warp + 1) * seg); i0 += 32) {
-              const int i = i0 + lane;
-              const unsigned tie = __ballot_sync(0xffffffffu, i < V && ordered(get(i)) == kmin);
-              if (before < keep && keep <= before + __popc(tie)) {
-                if (((tie >> lane) & 1u) && before + __popc(tie & ((2u << lane) - 1u)) == keep) s_pick[1] = full_key(kmin, i);
-              }
-              before += __popc(tie);
-            }
-          __syncthreads();
-          thr = s_pick[1];
-          __syncthreads();
-          return;
-        }
-        shift = max(0, 32 - __clz(kmax - kmin) - 11);
-        __syncthreads();
+        f(v, x);
       }
     };
-    __syncthreads();                           // (the table)
-    if (S.top_k > 0 && S.top_k < V) find(false);
-    if (S.top_p < 1.f) find(true);
-
-    // the running sum of the kept weights in the order of the indices: per warp's segment, then within the one that it passes the bound in
-    auto kept_weight = [&](int i) -> u64 {
-      if (i >= V) return 0;
-      const float x = get(i);
-      if (!(x > -INFINITY) || !W.eligible(x) || full_key(ordered(x), i) < thr) return 0;
-      return W(x);
-    };
     u64 sum = 0;
-    for (int i0 = warp * seg; i0 < min(V, (warp + 1) * seg); i0 += 32) sum += kept_weight(i0 + lane);
+    int last_bin = FINE;
+    float fine = 0.f;                          // bins of a unit of score; 0: no bins
+    if (by_mass || (use_k && S.top_k > NT)) {
+      // scores are counted by their distance from the largest (in the place of the list), and weighed where the bound goes by weight
+      unsigned* cnt = reinterpret_cast<unsigned*>(list);
+      const float range = fminf(W.cut, mx - bound);
+      fine = range > 1e-30f ? (float)FINE / range : 0.f;
+      for (int b = tid; b < FINE; b += NT) cnt[b] = 0;
+      __syncthreads();
+      each_vec([&](int v, const float* x) {
 #pragma unroll
-    for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
-    __syncthreads();
-    if (lane == 0) red[warp] = sum;
-    __syncthreads();
-    u64 total = 0;
+        for (int c = 0; c < VN; ++c) {
+          if (!(x[c] > -INFINITY) || !W.eligible(x[c])) continue;
+          if (by_mass) sum += W(x[c]);
+          if (x[c] >= bound) atomicAdd(cnt + (x[c] == mx ? 0 : min(FINE - 1, (int)((mx - x[c]) * fine))), 1u);
+        }
+      });
+      u64 wsum = sum;
 #pragma unroll
-    for (int w = 0; w < NW; ++w) total += red[w];
-    const float uf = P.u[row];
-    const double bound = (double)(uf >= 0.f ? fminf(uf, 0.99999994f) : 0.f) * (double)total;   // (NaN: 0)
-    int sw = NW - 1;
-    u64 before = 0, run = 0;
-    bool found = false;
-    for (int w = 0; w < NW; ++w) {
-      const u64 next = run + red[w];
-      if (!found && (double)next > bound) { sw = w; before = run; found = true; }
-      run = next;
+      for (int o = 16; o > 0; o >>= 1) wsum += __shfl_xor_sync(0xffffffffu, wsum, o);
+      __syncthreads();
+      if (lane == 0) red[warp] = wsum;
+      if (tid == 0) s_int[0] = FINE - 1;
+      __syncthreads();
+      mine.mass = 0;
+#pragma unroll
+      for (int w = 0; w < NW; ++w) mine.mass += red[w];
+      // the first bin down to which the share is reached: by count, or by what the scores weigh at least (2^40 the largest)
+      constexpr int PER = FINE / NT;
+      u64 part = 0, all;
+      const float step = fine > 0.f ? 1.f / (fine * S.temperature) : 0.f;
+      auto worth = [&](int b) { return by_mass ? (u64)(__expf(-(float)(b + 1) * step) * 0.9999f * 1099511627776.f) : 1ull; };
+#pragma unroll 4
+      for (int j = 0; j < PER; ++j) part += cnt[tid * PER + j] ? cnt[tid * PER + j] * worth(tid * PER + j) : 0;
+      u64 run = BlockOps<NT>::scan(part, red, all) - part;
+      const double share = by_mass ? (double)S.top_p * (double)mine.mass * ldexp(1.0, 40 - P.bits) : (double)((S.top_k + CL - 1) / CL);
+      if ((double)run < share && (double)(run + part) >= share) {
+#pragma unroll 1
+        for (int j = 0; j < PER; ++j) {
+          const u64 w = cnt[tid * PER + j] * worth(tid * PER + j);
+          if ((double)run < share && (double)(run + w) >= share) s_int[0] = tid * PER + j;
+          run += w;
+        }
+      }
+      __syncthreads();
+      mine.bin = s_int[0];
+      told = told_all[1];
+      tell(mine);
+      last_bin = 0;
+#pragma unroll
+      for (int c = 0; c < CL; ++c) last_bin = max(last_bin, told[c].bin);
     }
-    for (int i0 = sw * seg; i0 < min(V, (sw + 1) * seg); i0 += NT) {
-      u64 all;
-      const u64 w = kept_weight(i0 + tid < (sw + 1) * seg ? i0 + tid : V);
-      const u64 incl = BlockOps<NT>::scan(w, red, all);
-      if (tid == 0) s_int[0] = -1;
+    if (tid == 0) s_int[1] = 0;
+    __syncthreads();
+    each_vec([&](int v, const float* x) {
+        unsigned hits = 0;
+#pragma unroll
+        for (int c = 0; c < VN; ++c) {
+          const bool on = x[c] > -INFINITY && W.eligible(x[c]);
+          if (!listed) { if (on) sum += W(x[c]); }
+          else if (on && x[c] >= bound && (fine == 0.f || x[c] == mx || min(FINE - 1, (int)((mx - x[c]) * fine)) <= last_bin)) hits |= 1u << c;
+        }
+        if (listed && __any_sync(0xffffffffu, hits != 0)) {
+          const int cnt = __popc(hits);
+          int at = cnt;
+#pragma unroll
+          for (int o = 1; o < 32; o <<= 1) { const int y = __shfl_up_sync(0xffffffffu, at, o); if (lane >= o) at += y; }
+          int from = 0;
+          if (lane == 31) from = atomicAdd(s_int + 1, at);
+          at += __shfl_sync(0xffffffffu, from, 31) - cnt;
+#pragma unroll
+          for (int c = 0; c < VN; ++c)
+            if ((hits >> c) & 1u) { if (at < P.list) list[at] = full_key(ordered(x[c]), lo + v * VN + c - sh); ++at; }
+        }
+      });
+    u64 wsum = sum;                            // this warp's
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) wsum += __shfl_xor_sync(0xffffffffu, wsum, o);
+    __syncthreads();
+    if (lane == 0) red[warp] = wsum;
+    __syncthreads();
+    mine.mass = 0;
+#pragma unroll
+    for (int w = 0; w < NW; ++w) mine.mass += red[w];
+    mine.count = s_int[1];
+    told = told_all[2];
+    tell(mine);
+    u64 mass_all = 0, mass_before = 0;
+    int count = 0, at0 = 0;
+#pragma unroll
+    for (int c = 0; c < CL; ++c) {
+      if (c < rank) { mass_before += told[c].mass; at0 += told[c].count; }
+      mass_all += told[c].mass; count += told[c].count;
+    }
+    if (count > P.list) whole = true;
+    if (!listed) {
+      // no list: the CTA, the warp and the thread in whose part the running sum passes the bound
+      const double goal = (double)u * (double)mass_all;
+      writer = !((double)mass_before > goal) && (double)(mass_before + mine.mass) > goal;
+      if (writer) {
+        u64 run = mass_before;
+        int sw = NW - 1;
+        u64 before = 0;
+        bool found = false;
+#pragma unroll
+        for (int w = 0; w < NW; ++w) {
+          const u64 next = run + red[w];
+          if (!found && (double)next > goal) { sw = w; before = run; found = true; }
+          run = next;
+        }
+        const int e_end = min(vecs, (sw + 1) * wv);
+        if (tid == 0) s_int[0] = -1;
+        for (int v0 = sw * wv; v0 < e_end; v0 += NT) {
+          float x[VN];
+          u64 w[VN], part = 0, all;
+          const int v = v0 + tid;
+          if (v < e_end) vec(v, x);
+#pragma unroll
+          for (int c = 0; c < VN; ++c) {
+            w[c] = v < e_end && x[c] > -INFINITY && W.eligible(x[c]) ? W(x[c]) : 0;
+            part += w[c];
+          }
+          u64 c0 = before + BlockOps<NT>::scan(part, red, all) - part;
+#pragma unroll
+          for (int c = 0; c < VN; ++c) {
+            if (!((double)c0 > goal) && (double)(c0 + w[c]) > goal) s_int[0] = lo + v * VN + c - sh;
+            c0 += w[c];
+          }
+          __syncthreads();
+          token = s_int[0];
+          if (token >= 0) break;
+          before += all;
+        }
+      }
+    } else {
+      if (!whole && CL > 1) {                  // the lists to the first CTA
+        if (rank > 0)
+          for (int j = tid; j < mine.count; j += NT) {
+            uint32_t at;
+            asm volatile("mapa.shared::cluster.u32 %0, %1, 0;" : "=r"(at) : "r"(smem_addr(list + at0 + j)));
+            asm volatile("st.shared::cluster.u64 [%0], %1;" ::"r"(at), "l"(list[j]) : "memory");
+          }
+        asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+      }
+      if (rank > 0) return;
+      u64 thr = 0;                             // kept: keys from here up
+      // each(f): f(key) for every token in question, a key of 0 for none, the same number of calls in all threads of a warp
+      auto each_listed = [&](auto&& f) { for (int j0 = warp * 32; j0 < count; j0 += NT) f(j0 + lane < count ? list[j0 + lane] : 0ull); };
+      auto each_row = [&](auto&& f) {
+        for (int i0 = warp * 32; i0 < V; i0 += NT) {
+          const int i = i0 + lane;
+          const float x = i < V ? clean(to_f32(CL == 1 && STAGED ? xs[i + sh] : logits[i])) : -INFINITY;
+          f(x > -INFINITY && W.eligible(x) ? full_key(ordered(x), i) : 0ull);
+        }
+      };
+      auto score = [](u64 key) { return unordered((uint32_t)(key >> 32)); };
+
+      // Lowers `thr` to the first tokens whose count (mass: weight) reaches a bound: a histogram of the scores, its bin where the bound is
+      // passed, then that bin's elements, finer again while they are many.  mass_given: what all weigh, if known.
+      auto find = [&](auto&& each, const bool mass, const u64 mass_given) {
+        const float fscale = (float)NB / W.cut;   // (W.cut is between 1e-6 and 4e7)
+        uint32_t kmin = 0u, kmax = 0xffffffffu;   // ordered scores of the current interval
+        int shift = -1;                           // < 0: bins are linear in the score
+        u64 base = 0;
+        double target = mass ? (double)S.top_p * (double)mass_given : (double)S.top_k;
+        for (bool top = true;; top = false) {
+          auto bin_of = [&](uint32_t o) { const float x = unordered(o); return shift < 0 ? (x == mx ? 0 : min(NB - 1, (int)((mx - x) * fscale))) : (int)((kmax - o) >> shift); };
+          for (int b = tid; b < NB; b += NT) hist[b] = 0;
+          if (tid == 0) { s_int[0] = NB - 1; s_pick[0] = 0; }
+          __syncthreads();
+          each([&](u64 key) {
+            const uint32_t o = (uint32_t)(key >> 32);
+            if (key && o >= kmin && o <= kmax && key >= thr) {
+              const u64 w = mass ? W(score(key)) : 1;
+              if (w) atomicAdd(hist + bin_of(o), w);
+            }
+          });
+          __syncthreads();
+          u64 c[NB / NT], sum = 0, total;
+#pragma unroll
+          for (int j = 0; j < NB / NT; ++j) { c[j] = hist[tid * (NB / NT) + j]; sum += c[j]; }
+          u64 before = BlockOps<NT>::scan(sum, red, total) - sum;
+          if (top && mass && !mass_given) target = (double)S.top_p * (double)total;
+          if (top && !mass && (double)total <= target) return;   // no more than that: all stay
+#pragma unroll
+          for (int j = 0; j < NB / NT; ++j) {
+            if ((double)(base + before) < target && !((double)(base + before + c[j]) < target)) { s_int[0] = tid * (NB / NT) + j; s_pick[0] = before; }
+            before += c[j];
+          }
+          if (tid == 0) { s_int[1] = 0; s_int[2] = -1; s_int[3] = 0; }   // elements of the bin; smallest and largest score (as unsigned)
+          __syncthreads();
+          const int bin = s_int[0];
+          base += s_pick[0];
+          uint32_t omin = 0xffffffffu, omax = 0u;
+          u64* few = hist;                       // (the histogram has been read)
+          each([&](u64 key) {
+            const uint32_t o = (uint32_t)(key >> 32);
+            if (key && o >= kmin && o <= kmax && key >= thr && bin_of(o) == bin) {
+              const int at = atomicAdd(s_int + 1, 1);
+              if (at < SMALL) few[at] = key;
+              omin = min(omin, o); omax = max(omax, o);
+            }
+          });
+          omin = __reduce_min_sync(0xffffffffu, omin); omax = __reduce_max_sync(0xffffffffu, omax);
+          if (lane == 0 && omin <= omax) { atomicMin(reinterpret_cast<unsigned*>(s_int + 2), omin); atomicMax(reinterpret_cast<unsigned*>(s_int + 3), omax); }
+          __syncthreads();
+          const int nb = s_int[1];
+          kmin = (uint32_t)s_int[2]; kmax = (uint32_t)s_int[3];
+          if (nb <= SMALL) {
+            if (tid < nb) small_w[tid] = mass ? W(score(few[tid])) : 1;
+            if (tid == 0) s_pick[1] = ~0ull;
+            __syncthreads();
+            if (tid < nb) {
+              const u64 key = few[tid];
+              u64 above = 0;
+              for (int j = 0; j < nb; ++j) above += few[j] > key ? small_w[j] : 0;
+              if ((double)(base + above) < target) atomicMin(s_pick + 1, key);
+            }
+            __syncthreads();
+            thr = s_pick[1];
+            __syncthreads();
+            return;
+          }
+          if (kmin == kmax) {
+            // equal scores: the first of them by index, as many as the bound needs
+            const u64 w = mass ? W(unordered(kmin)) : 1;
+            u64 keep = w ? (u64)((target - (double)base) / (double)w) : 0;
+            if (keep > 0) --keep;
+            while ((double)(base + keep * w) < target && keep < (u64)nb) ++keep;   // (the division may be off by one)
+            if (keep == 0) keep = 1;
+            // the keep-th lowest index: bit by bit
+            uint32_t prefix = 0;
+            u64 left = keep;
+            for (int bit = 20; bit >= 0; --bit) {
+              if (tid == 0) s_int[1] = 0;
+              __syncthreads();
+              int cnt = 0;                       // ties with this prefix and a zero in this bit
+              each([&](u64 key) {
+                const uint32_t idx = ~(uint32_t)key;
+                if (key && (uint32_t)(key >> 32) == kmin && key >= thr && (idx >> bit) == (prefix >> bit)) ++cnt;
+              });
+              cnt = __reduce_add_sync(0xffffffffu, cnt);
+              if (lane == 0 && cnt) atomicAdd(s_int + 1, cnt);
+              __syncthreads();
+              const int zeros = s_int[1];
+              __syncthreads();
+              if ((u64)zeros < left) { left -= zeros; prefix |= 1u << bit; }
+            }
+            thr = full_key(kmin, (int)prefix);
+            return;
+          }
+          shift = max(0, 32 - __clz(kmax - kmin) - (31 - __clz(NB)));   // (NB bins cover the interval)
+          __syncthreads();
+        }
+      };
+      // the token: kept weights in the order of the indices - a histogram over the indices, then the bin's tokens one against another
+      auto drawn = [&](auto&& each) {
+        int shift = 0;
+        while (((V - 1) >> shift) >= NB) ++shift;
+        for (int b = tid; b < NB; b += NT) hist[b] = 0;
+        __syncthreads();
+        each([&](u64 key) {
+          if (key && key >= thr) {
+            const u64 w = W(score(key));
+            if (w) atomicAdd(hist + (~(uint32_t)key >> shift), w);
+          }
+        });
+        __syncthreads();
+        u64 c[NB / NT], sum = 0, total;
+#pragma unroll
+        for (int j = 0; j < NB / NT; ++j) { c[j] = hist[tid * (NB / NT) + j]; sum += c[j]; }
+        u64 before = BlockOps<NT>::scan(sum, red, total) - sum;
+        const double goal = (double)u * (double)total;
+#pragma unroll
+        for (int j = 0; j < NB / NT; ++j) {
+          if (!((double)before > goal) && (double)(before + c[j]) > goal) { s_int[0] = tid * (NB / NT) + j; s_pick[0] = before; }
+          before += c[j];
+        }
+        if (tid == 0) { s_int[1] = 0; s_int[2] = -1; }
+        __syncthreads();
+        const int bin = s_int[0];
+        const u64 base = s_pick[0];
+        u64* few = hist;                         // (at most vocab / NB <= NB tokens)
+        each([&](u64 key) {
+          if (key && key >= thr && (int)(~(uint32_t)key >> shift) == bin) few[atomicAdd(s_int + 1, 1)] = key;
+        });
+        __syncthreads();
+        const int nb = s_int[1];
+        for (int a = tid; a < nb; a += NT) {
+          const uint32_t idx = ~(uint32_t)few[a];
+          const u64 w = W(score(few[a]));
+          u64 run = base;
+          for (int j = 0; j < nb; ++j) if (~(uint32_t)few[j] < idx) run += W(score(few[j]));
+          if (!((double)run > goal) && (double)(run + w) > goal) s_int[2] = (int)idx;
+        }
+        __syncthreads();
+        token = s_int[2];
+      };
+      // a few dozen tokens: ranked one against another, one thread each
+      auto drawn_small = [&]() {
+        const bool on = tid < count;
+        const u64 key = on ? list[tid] : 0;
+        u64 w = on ? W(score(key)) : 0;
+        auto sum_over = [&](auto&& pick) { u64 r = 0; for (int j = 0; j < count; ++j) r += pick(list[j]) ? small_w[j] : 0; return r; };
+        if (use_k && on) {
+          int above = 0;
+          for (int j = 0; j < count; ++j) above += list[j] > key;
+          if (above >= S.top_k) w = 0;
+        }
+        if (on) small_w[tid] = w;
+        __syncthreads();
+        if (use_p) {
+          bool keep = false;
+          if (on) {
+            const u64 all = use_k ? sum_over([](u64) { return true; }) : mass_all;
+            keep = (double)sum_over([&](u64 o) { return o > key; }) < (double)S.top_p * (double)all;
+          }
+          __syncthreads();
+          if (on && !keep) small_w[tid] = w = 0;
+          __syncthreads();
+        }
+        if (on) {
+          const double goal = (double)u * (double)sum_over([](u64) { return true; });
+          const u64 before = sum_over([&](u64 o) { return (uint32_t)o > (uint32_t)key; });   // (the low word is the index's complement)
+          if (!((double)before > goal) && (double)(before + w) > goal) s_int[2] = (int)~(uint32_t)key;
+        }
+        __syncthreads();
+        token = s_int[2];
+      };
       __syncthreads();
-      if ((double)(before + incl) > bound && !((double)(before + incl - w) > bound)) s_int[0] = i0 + tid;
-      __syncthreads();
-      token = s_int[0];
-      if (token >= 0) break;
-      before += all;
+      if (!whole && count <= SMALL) drawn_small();
+      else if (whole) {
+        if (use_k) find(each_row, false, 0);
+        if (use_p) find(each_row, true, 0);
+        drawn(each_row);
+      } else {
+        if (use_k) find(each_listed, false, 0);
+        if (use_p) find(each_listed, true, use_k ? 0 : mass_all);
+        drawn(each_listed);
+      }
     }
   }
-  if (tid == 0) {
+  if (writer && tid == 0) {
     P.tokens[(size_t)req * (P.k_max + 1) + r_in] = token;
     if (P.k[req] == 0) P.accept[req] = 0;
   }
@@ -330,19 +658,35 @@ __global__ void k_sample_accept(const __grid_constant__ SampleParams P) {
   P.accept[i] = a;
 }
 
-template <typename T, int NT, bool STAGED> int launch_rows(const SampleParams& P, size_t smem, cudaStream_t st) {
-  auto kern = k_sample<T, NT, STAGED>;
-  if (smem > 48 * 1024) SCK(cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, 227 * 1024 - 2048));
-  kern<<<P.n_rows, NT, smem, st>>>(P);
-  SCK(cudaGetLastError());
+constexpr size_t SP_ROOM = 112 * 1024, SP_MOST = 227 * 1024 - 4096;
+template <typename T, int CL, bool STAGED> int launch_rows(SampleParams& P, cudaStream_t st) {
+  auto kern = k_sample<T, CL, STAGED>;
+  // the list takes what is left: of half an SM, or of a whole one where the slice needs more
+  const size_t least = sp_smem<T>(P.vocab, CL, STAGED, FINE / 2), room = least <= SP_ROOM ? SP_ROOM : SP_MOST;
+  P.list = FINE / 2 + (int)((room - least) / 8);
+  const size_t smem = sp_smem<T>(P.vocab, CL, STAGED, P.list);
+  SCK(cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)SP_MOST));
+  cudaLaunchConfig_t cfg{};
+  cfg.gridDim = dim3(P.n_rows * CL); cfg.blockDim = dim3(SP_THREADS); cfg.dynamicSmemBytes = smem; cfg.stream = st;
+  cudaLaunchAttribute at[1];
+  at[0].id = cudaLaunchAttributeClusterDimension;
+  at[0].val.clusterDim.x = CL; at[0].val.clusterDim.y = 1; at[0].val.clusterDim.z = 1;
+  cfg.attrs = at; cfg.numAttrs = CL > 1 ? 1 : 0;
+  SCK(cudaLaunchKernelEx(&cfg, kern, P));
   return STAIRS_OK;
 }
 
-template <typename T> int launch_sample(const SampleParams& P, cudaStream_t st) {
-  const size_t fixed = (size_t)NB * 8 + SMALL * 16 + 64 * 8, row = (size_t)P.vocab * sizeof(T);
-  const bool staged = fixed + row <= 227 * 1024 - 2048;
-  if (staged) return sizeof(T) == 4 ? launch_rows<T, 1024, true>(P, fixed + row, st) : launch_rows<T, 512, true>(P, fixed + row, st);
-  return launch_rows<T, 512, false>(P, fixed, st);
+// CTAs a row: as many as keep two CTAs on every SM while the rows are few, and as the slices need to fit.
+template <typename T> int launch_sample(SampleParams& P, cudaStream_t st) {
+  int cl = 1;
+  while (cl < 8 && (P.n_rows * cl * 2 <= 2 * 148 || sp_smem<T>(P.vocab, cl, true, FINE / 2) > SP_ROOM)) cl *= 2;
+  if (sp_smem<T>(P.vocab, cl, true, FINE / 2) > SP_MOST) return launch_rows<T, 8, false>(P, st);
+  switch (cl) {
+    case 1: return launch_rows<T, 1, true>(P, st);
+    case 2: return launch_rows<T, 2, true>(P, st);
+    case 4: return launch_rows<T, 4, true>(P, st);
+    default: return launch_rows<T, 8, true>(P, st);
+  }
 }
 
 }  // namespace
