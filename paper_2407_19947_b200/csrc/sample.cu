@@ -34,58 +34,83 @@ __device__ __forceinline__ uint32_t ordered(float x) {
 __device__ __forceinline__ float unordered(uint32_t o) { return __uint_as_float((o & 0x80000000u) ? (o & 0x7fffffffu) : ~o); }
 __device__ __forceinline__ u64 full_key(uint32_t o, int i) { return ((u64)o << 32) | (uint32_t)~i; }
 
-// 2^bits exp((x - m) / T), rounded to a whole number.  exp by a table of 2^(j/64) and a polynomial of the rest (P. Tang, "Table-driven
-// implementation of the exponential function in IEEE floating-point arithmetic", 1989): |r| <= ln 2 / 128, so its fourth-degree
-// Taylor polynomial is off by at most 4e-14.
+// 2^bits exp((x - m) / T), rounded to a whole number.  exp by a table of 2^(j/16) and a polynomial of the rest (P. Tang, "Table-driven
+// implementation of the exponential function in IEEE floating-point arithmetic", 1989): |f| <= 1/2 sixteenth of an octave, so its
+// fifth-degree Taylor polynomial is off by at most 1.5e-13.  Sixteen entries of 8 bytes are a word in every bank: no conflicts.
 struct Weigher {
-  double m, inv_t, min_w;
-  float mf, cut;
-  const double* tab;                          // 2^(bits + j/64)
-  __device__ __forceinline__ bool eligible(float x) const { return x == mf || mf - x <= cut; }   // (never NaN or -infinity; anything else weighs 0)
+  double m, inv_t16;                          // inv_t16: sixteenths of an octave per unit of score
+  float mf, cut, least;                       // least: the smallest score that may weigh anything
+  u64 min_w;
+  const double* tab;                          // 2^(bits + j/16)
+  __device__ __forceinline__ bool eligible(float x) const { return x >= least; }   // (never NaN or -infinity; anything else weighs 0)
+  // 32 to 64 bits in integer instructions (conversions run at a quarter of the rate of 64-bit additions); a score below 2^-126 comes out
+  // within 2^-126, infinity as 2^128
+  static __device__ __forceinline__ double widen(float x) {
+    const uint32_t u = __float_as_uint(x);
+    return __hiloint2double((int)((u & 0x80000000u) | (((u & 0x7fffffffu) >> 3) + 0x38000000u)), (int)(u << 29));
+  }
   __device__ __forceinline__ u64 operator()(float x) const {
-    const double t = x == mf ? 0.0 : ((double)x - m) * inv_t;
-    constexpr double MAGIC = 6755399441055744.0, LN2 = 0.69314718055994530942;   // 1.5 * 2^52: adding it rounds to a whole number
-    const double z = fma(t, 64.0 / LN2, MAGIC);
+    const double y = (widen(x) - m) * inv_t16;
+    constexpr double MAGIC = 6755399441055744.0, C = 0.69314718055994530942 / 16.0;   // 1.5 * 2^52: adding it rounds to a whole number
+    const double z = y + MAGIC;
     const int n = __double2loint(z);
-    const double r = fma(z - MAGIC, -LN2 / 64.0, t);
-    const double p = fma(fma(fma(fma(r, 1.0 / 24.0, 1.0 / 6.0), r, 0.5), r, 1.0), r, 1.0);
-    const double v = p * tab[n & 63];
-    const double w = __hiloint2double(__double2hiint(v) + ((n >> 6) << 20), __double2loint(v));
-    if (w < min_w) return 0;
-    return (u64)(__double_as_longlong(w + 4503599627370496.0) - 0x4330000000000000ll);   // + 2^52: the low bits are the whole number
+    const double f = y - (z - MAGIC);
+    const double p = fma(fma(fma(fma(fma(f, C * C * C * C * C / 120.0, C * C * C * C / 24.0), f, C * C * C / 6.0), f, C * C / 2.0), f, C), f, 1.0);
+    const double v = p * tab[n & 15];
+    const double w = __hiloint2double(__double2hiint(v) + ((n >> 4) << 20), __double2loint(v));
+    const u64 r = (u64)(__double_as_longlong(w + 4503599627370496.0) - 0x4330000000000000ll);   // + 2^52: the low bits are the whole number
+    return r >= min_w ? r : 0;
   }
 };
 
-template <int NT> struct BlockOps {
-  static constexpr int NW = NT / 32;
-  // inclusive running sum over the block's threads, and the sum of all; `red` holds NW + 1 numbers
-  static __device__ __forceinline__ u64 scan(u64 v, u64* red, u64& total) {
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+// inclusive running sum over a block of 512 threads, and the sum of all; `red` holds 16 numbers
+__device__ __forceinline__ u64 block_scan(u64 v, u64* red, u64* total) {
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
 #pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-      const u64 x = __shfl_up_sync(0xffffffffu, v, o);
-      if (lane >= o) v += x;
-    }
-    __syncthreads();
-    if (lane == 31) red[warp] = v;
-    __syncthreads();
-    u64 before = 0, all = 0;
-#pragma unroll
-    for (int w = 0; w < NW; ++w) { const u64 x = red[w]; all += x; if (w < warp) before += x; }
-    total = all;
-    return v + before;
+  for (int o = 1; o < 32; o <<= 1) {
+    const u64 x = __shfl_up_sync(0xffffffffu, v, o);
+    if (lane >= o) v += x;
   }
+  __syncthreads();
+  if (lane == 31) red[warp] = v;
+  __syncthreads();
+  u64 r = red[lane & 15];
+#pragma unroll
+  for (int o = 1; o < 16; o <<= 1) {
+    const u64 x = __shfl_up_sync(0xffffffffu, r, o);
+    if ((lane & 15) >= o) r += x;
+  }
+  *total = __shfl_sync(0xffffffffu, r, 15);
+  const u64 before = __shfl_sync(0xffffffffu, r, (warp + 15) & 15);
+  return v + (warp ? before : 0);
+}
+__device__ __forceinline__ u64 block_sum(u64 v, u64* red) {
+  u64 total;
+  block_scan(v, red, &total);
+  return total;
+}
+
+// Histograms of 64-bit numbers: shared memory adds 32 bits at a time by itself, 64 only in a loop of compare-and-swaps (2500 additions 28000 cycles,
+// as two halves with the carry read off the old value 2000).
+struct Hist {
+  unsigned* lo;                               // [NB] low words, then [NB] high words
+  __device__ __forceinline__ void clear() const { for (int b = threadIdx.x; b < 2 * NB; b += blockDim.x) lo[b] = 0; }
+  __device__ __forceinline__ void add(int b, u64 w) const {
+    const unsigned l = (unsigned)w, old = atomicAdd(lo + b, l), h = (unsigned)(w >> 32) + (old + l < old ? 1u : 0u);
+    if (h) atomicAdd(lo + NB + b, h);
+  }
+  __device__ __forceinline__ u64 at(int b) const { return (u64)lo[NB + b] << 32 | lo[b]; }
 };
 
 // What the CTAs of a row tell one another.
-struct Told { float m, bound, weight; int count, first, bin; u64 mass; };
+struct Told { float m, bound, weight; int count, first, bin; u64 mass, part; };
 
-constexpr int SP_THREADS = 512, FINE = 8192;   // FINE: bins of a count of scores, in the list's place (which so has FINE / 2 entries at least)
+constexpr int SP_THREADS = 512, FINE = 8192, LEAST_LIST = FINE / 2;   // FINE: bins of a count of scores, in the list's place (which so has LEAST_LIST entries at least)
 template <typename T> constexpr int sp_vec() { return 16 / sizeof(T); }
 // elements of a CTA's slice of the vocabulary, and its shared memory
 __host__ __device__ inline int sp_slice(int vocab, int cl) { return ((vocab + cl - 1) / cl + 63) / 64 * 64; }
 template <typename T> size_t sp_smem(int vocab, int cl, bool staged, int list) {
-  return (size_t)(NB + list + SMALL + 64) * 8 + (staged ? ((size_t)sp_slice(vocab, cl) + 2 * sp_vec<T>()) * sizeof(T) : 0);
+  return (size_t)(NB + list + SMALL + 16) * 8 + (staged ? ((size_t)sp_slice(vocab, cl) + 2 * sp_vec<T>()) * sizeof(T) : 0);
 }
 
 // One row: CL CTAs (a cluster where there are several), each with a slice of the vocabulary in shared memory.
@@ -93,7 +118,7 @@ template <typename T> size_t sp_smem(int vocab, int cl, bool staged, int list) {
 //     as large as the k-th of them, and scores of weight below (1 - top_p) / vocab of the weight that they have together are never in the
 //     first top_p of the whole (all such tokens together weigh less than the rest).
 //     Where that is not sharp - a top-p without a top-k, a top-k above 512 - scores above the bound are counted in 8192 bins, and the bound is
-//     the bin down to which a CTA holds its share of the count, or surely top_p of its own weight (each score taken for the smallest of its bin).
+//     the bin down to which there are k of them, or surely top_p of the whole weight (each score taken for the smallest of its bin).
 //  2. One pass: scores above the bound are listed; rows that need it are weighed as a whole.
 //  3. The first CTA gets the lists and filters and draws among a few dozen (ranked one against another) to some thousand tokens (by
 //     histograms).  Rows without top-k and top-p need no list: the running sum is looked up by CTA, warp and thread.  Rows whose list
@@ -102,14 +127,14 @@ template <typename T, int CL, bool STAGED>
 __global__ void __launch_bounds__(SP_THREADS, 2) k_sample(const __grid_constant__ SampleParams P) {
   constexpr int NT = SP_THREADS, NW = NT / 32, VN = sp_vec<T>();
   extern __shared__ __align__(16) unsigned char sp_sm[];
-  u64* hist = reinterpret_cast<u64*>(sp_sm);
-  u64* list = hist + NB;
+  const Hist hist{reinterpret_cast<unsigned*>(sp_sm)};
+  u64* list = reinterpret_cast<u64*>(sp_sm) + NB;
   u64* small_w = list + P.list;
   double* tab = reinterpret_cast<double*>(small_w + SMALL);
-  T* xs = reinterpret_cast<T*>(tab + 64);
+  T* xs = reinterpret_cast<T*>(tab + 16);
   __shared__ u64 red[NW + 1], s_pick[4];
   __shared__ int s_int[4];
-  __shared__ Told told_all[3][CL];            // (a set for each time: a fast CTA may send its next numbers while a slow one still reads the last)
+  __shared__ Told told_all[5][CL];            // (a set for each time: a fast CTA may send its next numbers while a slow one still reads the last)
   Told* told = told_all[0];
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, row = blockIdx.x / CL, rank = blockIdx.x % CL, V = P.vocab;
   launch_dependents();
@@ -124,7 +149,7 @@ __global__ void __launch_bounds__(SP_THREADS, 2) k_sample(const __grid_constant_
   const stairs_sampling S = P.s[req];
   const T* logits = reinterpret_cast<const T*>(P.logits) + (size_t)row * P.ld;
   const int slice = sp_slice(V, CL), lo = min(rank * slice, V), n = min(slice, V - lo);
-  if (tid < 64) tab[tid] = exp2((double)P.bits + tid / 64.0);
+  if (tid < 16) tab[tid] = exp2((double)P.bits + tid / 16.0);
   auto clean = [](float x) { return x == x ? x + 0.f : -INFINITY; };   // (NaN counts as -infinity, -0 as 0)
 
   // The slice in whole vectors from the first 16-byte boundary at or before it; what is outside of it reads as -infinity.
@@ -137,11 +162,17 @@ __global__ void __launch_bounds__(SP_THREADS, 2) k_sample(const __grid_constant_
       for (int c = 0; c < VN; ++c) { const int i = v * VN + c; e[c] = i >= sh && i < sh + n ? base[i] : from_f32<T>(-INFINITY); }
     }
   };
-  auto vec = [&](int v, float* x) {                 // the same, cleaned, for the passes behind the first
-    alignas(16) T e[VN];
+  auto vec = [&](int v, T* e) {                     // the same for the passes behind the first
     if (STAGED) *reinterpret_cast<uint4*>(e) = *(reinterpret_cast<const uint4*>(xs) + v); else load(v, e);
-#pragma unroll
-    for (int c = 0; c < VN; ++c) x[c] = clean(to_f32(e[c]));
+  };
+  auto largest = [](const T* e) {                   // of a vector (NaN is passed over)
+    if constexpr (std::is_same<T, float>::value) return fmaxf(fmaxf(e[0], e[1]), fmaxf(e[2], e[3]));
+    else {
+      typedef typename std::conditional<std::is_same<T, bf16>::value, __nv_bfloat162, __half2>::type T2;
+      const T2* p = reinterpret_cast<const T2*>(e);
+      const T2 m = __hmax2(__hmax2(p[0], p[1]), __hmax2(p[2], p[3]));
+      return to_f32(__hmax(m.x, m.y));
+    }
   };
   float tmax = -INFINITY;
   {
@@ -154,8 +185,7 @@ __global__ void __launch_bounds__(SP_THREADS, 2) k_sample(const __grid_constant_
       for (int j = 0; j < UN; ++j)
         if (v0 + j * NT < vecs) {
           if (STAGED) *(reinterpret_cast<uint4*>(xs) + v0 + j * NT) = *reinterpret_cast<uint4*>(e[j]);
-#pragma unroll
-          for (int c = 0; c < VN; ++c) tmax = fmaxf(tmax, to_f32(e[j][c]));   // (NaN is passed over)
+          tmax = fmaxf(tmax, largest(e[j]));
         }
     }
     tmax += 0.f;
@@ -165,22 +195,18 @@ __global__ void __launch_bounds__(SP_THREADS, 2) k_sample(const __grid_constant_
     __syncthreads();
     if (lane == 0) red[warp] = ((u64)a << 32) | b;
     __syncthreads();
-    uint32_t A = 0u, B = 0xffffffffu;
-#pragma unroll
-    for (int w = 0; w < NW; ++w) { A = max(A, (uint32_t)(red[w] >> 32)); B = min(B, (uint32_t)red[w]); }
-    mx = unordered(A); mn = unordered(B);
+    const u64 r = red[lane & 15];
+    mx = unordered(__reduce_max_sync(0xffffffffu, (uint32_t)(r >> 32))); mn = unordered(__reduce_min_sync(0xffffffffu, (uint32_t)r));
   };
   auto tell = [&](const Told& t) {                  // this CTA's numbers to all; then `told` is complete
-    if (CL == 1) {
-      if (tid == 0) told[0] = t;
-      __syncthreads();
-    } else {
-      if (tid < CL) {
+    if (tid == 0) told[rank] = t;
+    __syncthreads();
+    if (CL > 1) {
+      constexpr int WORDS = sizeof(Told) / 4;        // a thread a word and CTA
+      if (tid < CL * WORDS && tid / WORDS != rank) {
         uint32_t at;
-        asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"(smem_addr(told + rank)), "r"(tid));
-        const uint32_t* w = reinterpret_cast<const uint32_t*>(&t);
-#pragma unroll
-        for (int i = 0; i < (int)sizeof(Told) / 4; ++i) asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(at + 4 * i), "r"(w[i]) : "memory");
+        asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"(smem_addr(told + rank) + 4 * (tid % WORDS)), "r"(tid / WORDS));
+        asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(at), "r"(reinterpret_cast<const uint32_t*>(told + rank)[tid % WORDS]) : "memory");
       }
       asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
     }
@@ -202,15 +228,15 @@ __global__ void __launch_bounds__(SP_THREADS, 2) k_sample(const __grid_constant_
         mine.bound = mn;
         if (range > 1e-30f && range < INFINITY) {
           const float scale = (float)NB / range;
-          for (int b = tid; b < NB; b += NT) hist[b] = 0;
+          hist.clear();
           __syncthreads();
           const int bin = tmax > -INFINITY ? min(NB - 1, (int)((mine.m - tmax) * scale)) : NB;
-          if (bin < NB) atomicAdd(reinterpret_cast<unsigned*>(hist + bin), 1u);
+          if (bin < NB) hist.add(bin, 1);
           __syncthreads();
           u64 c[NB / NT], sum = 0, all;
 #pragma unroll
-          for (int j = 0; j < NB / NT; ++j) { c[j] = hist[tid * (NB / NT) + j]; sum += c[j]; }
-          u64 before = BlockOps<NT>::scan(sum, red, all) - sum;
+          for (int j = 0; j < NB / NT; ++j) { c[j] = hist.at(tid * (NB / NT) + j); sum += c[j]; }
+          u64 before = block_scan(sum, red, &all) - sum;
 #pragma unroll
           for (int j = 0; j < NB / NT; ++j) {
             if (before < (u64)S.top_k && before + c[j] >= (u64)S.top_k) s_int[0] = tid * (NB / NT) + j;
@@ -224,14 +250,7 @@ __global__ void __launch_bounds__(SP_THREADS, 2) k_sample(const __grid_constant_
       }
     } else if (use_p && !use_k) {
       float w = tmax == mine.m ? 1.f : __expf((tmax - mine.m) / S.temperature);
-      w = warp_sum(w);
-      __syncthreads();
-      if (lane == 0) red[warp] = __float_as_uint(w);
-      __syncthreads();
-      float sum = 0.f;
-#pragma unroll
-      for (int i = 0; i < NW; ++i) sum += __uint_as_float((uint32_t)red[i]);
-      mine.weight = sum;
+      mine.weight = (float)block_sum((u64)(unsigned)(w * 65536.f), red) * (1.f / 65536.f);   // (rounded down: a bound needs no more)
     }
   }
   tell(mine);
@@ -246,18 +265,17 @@ __global__ void __launch_bounds__(SP_THREADS, 2) k_sample(const __grid_constant_
     int best = 0x7fffffff;
     if (mine.m == mx)
       for (int v = tid; v < vecs; v += NT) {
-        float x[VN];
-        vec(v, x);
+        alignas(16) T e[VN];
+        vec(v, e);
+        if (largest(e) != mx) continue;
 #pragma unroll
-        for (int c = VN - 1; c >= 0; --c) if (x[c] == mx) best = min(best, lo + v * VN + c - sh);
-        if (best < 0x7fffffff) break;
+        for (int c = VN - 1; c >= 0; --c) if (to_f32(e[c]) == mx) best = min(best, lo + v * VN + c - sh);
       }
     best = __reduce_min_sync(0xffffffffu, best);
     __syncthreads();
     if (lane == 0) red[warp] = (u64)best;
     __syncthreads();
-#pragma unroll
-    for (int w = 0; w < NW; ++w) best = min(best, (int)red[w]);
+    best = __reduce_min_sync(0xffffffffu, (int)red[lane & 15]);
     mine.first = best;
     told = told_all[1];
     tell(mine);
@@ -265,12 +283,13 @@ __global__ void __launch_bounds__(SP_THREADS, 2) k_sample(const __grid_constant_
     for (int c = 0; c < CL; ++c) best = min(best, told[c].first);
     token = best;
   } else {
-    Weigher W;
-    W.mf = mx; W.m = (double)mx; W.inv_t = 1.0 / (double)S.temperature; W.tab = tab;
-    W.min_w = S.min_p > 0.f ? ldexp((double)S.min_p, P.bits) : 0.0;
     // what may weigh anything: scores not much further than this below the largest
     const float nats = S.min_p > 0.f ? fminf(-logf(S.min_p) + 1e-3f, (P.bits + 1.5f) * 0.6931472f) : (P.bits + 1.5f) * 0.6931472f;
+    Weigher W;
+    W.mf = mx; W.m = Weigher::widen(mx); W.inv_t16 = 16.0 / 0.69314718055994530942 / (double)S.temperature; W.tab = tab;
+    W.min_w = (u64)ceil((double)S.min_p * (double)(1ull << P.bits));
     W.cut = nats * S.temperature * 1.00001f;
+    W.least = mx - W.cut;                      // (rounded: the next score below is further than `cut` away all the same; +infinity: itself alone)
     const float uf = P.u[row];
     const float u = uf >= 0.f ? fminf(uf, 0.99999994f) : 0.f;   // (NaN: 0)
     bool whole = false;                        // the first CTA works on the whole row
@@ -285,19 +304,6 @@ __global__ void __launch_bounds__(SP_THREADS, 2) k_sample(const __grid_constant_
     }
     const int wv = (vecs + NW - 1) / NW, v_end = min(vecs, (warp + 1) * wv);   // a warp's vectors lie together: sums in the order of the indices
     const bool listed = use_k || use_p;
-    // each_vec(f): f(v, x, on) for this warp's vectors, 32 at a time (on: it exists)
-    auto each_vec = [&](auto&& f) {
-      for (int v0 = warp * wv; v0 < v_end; v0 += 32) {
-        const int v = v0 + lane;
-        float x[VN];
-        if (v < v_end) vec(v, x);
-        else {
-#pragma unroll
-          for (int c = 0; c < VN; ++c) x[c] = -INFINITY;
-        }
-        f(v, x);
-      }
-    };
     u64 sum = 0;
     int last_bin = FINE;
     float fine = 0.f;                          // bins of a unit of score; 0: no bins
@@ -308,83 +314,121 @@ __global__ void __launch_bounds__(SP_THREADS, 2) k_sample(const __grid_constant_
       fine = range > 1e-30f ? (float)FINE / range : 0.f;
       for (int b = tid; b < FINE; b += NT) cnt[b] = 0;
       __syncthreads();
-      each_vec([&](int v, const float* x) {
+      for (int v = warp * wv + lane; v < v_end; v += 32) {
+        alignas(16) T e[VN];
+        vec(v, e);
+        if (!by_mass && !W.eligible(largest(e))) continue;
 #pragma unroll
         for (int c = 0; c < VN; ++c) {
-          if (!(x[c] > -INFINITY) || !W.eligible(x[c])) continue;
-          if (by_mass) sum += W(x[c]);
-          if (x[c] >= bound) atomicAdd(cnt + (x[c] == mx ? 0 : min(FINE - 1, (int)((mx - x[c]) * fine))), 1u);
+          const float x = to_f32(e[c]);
+          if (!W.eligible(x)) continue;
+          if (by_mass) sum += W(x);
+          if (x >= bound) atomicAdd(cnt + (x == mx ? 0 : min(FINE - 1, (int)((mx - x) * fine))), 1u);
         }
-      });
-      u64 wsum = sum;
+      }
+      mine.mass = by_mass ? block_sum(sum, red) : 0;
+      told = told_all[1];
+      tell(mine);                              // (and every CTA's counts are complete)
+      u64 mass = 0;
 #pragma unroll
-      for (int o = 16; o > 0; o >>= 1) wsum += __shfl_xor_sync(0xffffffffu, wsum, o);
-      __syncthreads();
-      if (lane == 0) red[warp] = wsum;
-      if (tid == 0) s_int[0] = FINE - 1;
-      __syncthreads();
-      mine.mass = 0;
+      for (int c = 0; c < CL; ++c) mass += told[c].mass;
+      // the first bin down to which the filter's bound is reached: by count, or by what the scores weigh at least (2^32 the largest; a bin's
+      // weight from that of the one before it: a few roundings of 2^-24, for which 1e-4 is taken off); a CTA takes its share of the bins, of all CTAs
+      constexpr int PER = FINE / CL / NT;
+      const int bin0 = (rank * NT + tid) * PER;
+      const float step = fine > 0.f ? 1.f / (fine * S.temperature) : 0.f, q = by_mass ? __expf(-step) : 1.f;
+      const float w0 = by_mass ? __expf(-(float)(bin0 + 1) * step) * 0.9999f * 4294967296.f : 1.f;
+      unsigned c[PER];
 #pragma unroll
-      for (int w = 0; w < NW; ++w) mine.mass += red[w];
-      // the first bin down to which the share is reached: by count, or by what the scores weigh at least (2^40 the largest)
-      constexpr int PER = FINE / NT;
-      u64 part = 0, all;
-      const float step = fine > 0.f ? 1.f / (fine * S.temperature) : 0.f;
-      auto worth = [&](int b) { return by_mass ? (u64)(__expf(-(float)(b + 1) * step) * 0.9999f * 1099511627776.f) : 1ull; };
-#pragma unroll 4
-      for (int j = 0; j < PER; ++j) part += cnt[tid * PER + j] ? cnt[tid * PER + j] * worth(tid * PER + j) : 0;
-      u64 run = BlockOps<NT>::scan(part, red, all) - part;
-      const double share = by_mass ? (double)S.top_p * (double)mine.mass * ldexp(1.0, 40 - P.bits) : (double)((S.top_k + CL - 1) / CL);
-      if ((double)run < share && (double)(run + part) >= share) {
-#pragma unroll 1
-        for (int j = 0; j < PER; ++j) {
-          const u64 w = cnt[tid * PER + j] * worth(tid * PER + j);
-          if ((double)run < share && (double)(run + w) >= share) s_int[0] = tid * PER + j;
-          run += w;
+      for (int j = 0; j < PER; ++j) c[j] = 0;
+#pragma unroll
+      for (int r = 0; r < CL; ++r) {
+        uint32_t from = smem_addr(cnt + bin0);
+        if (CL > 1) asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(from) : "r"(from), "r"(r));
+#pragma unroll
+        for (int j = 0; j < PER; j += 2) {
+          unsigned x, y;
+          if (CL > 1) asm volatile("ld.shared::cluster.v2.u32 {%0, %1}, [%2];" : "=r"(x), "=r"(y) : "r"(from + 4 * j) : "memory");
+          else asm volatile("ld.shared.v2.u32 {%0, %1}, [%2];" : "=r"(x), "=r"(y) : "r"(from + 4 * j) : "memory");
+          c[j] += x; c[j + 1] += y;
         }
+      }
+      float part = 0.f, w = w0;
+#pragma unroll
+      for (int j = 0; j < PER; ++j) { part += (float)c[j] * w; w *= q; }
+      const double share = by_mass ? (double)S.top_p * (double)mass * (4294967296.0 / (double)(1ull << P.bits)) : (double)S.top_k;
+      u64 upto = block_scan((u64)part, red, &mine.part);
+      if (tid == 0) s_int[0] = -1;
+      told = told_all[2];
+      tell(mine);                              // (and every CTA has read the counts)
+#pragma unroll
+      for (int r = 0; r < CL; ++r) if (r < rank) upto += told[r].part;
+      const u64 run0 = upto - (u64)part;
+      if ((double)run0 < share && (double)upto >= share) {
+        const float left = (float)(share - (double)run0);
+        float run = 0.f;
+        int bin = bin0;
+        w = w0;
+#pragma unroll
+        for (int j = 0; j < PER; ++j) { run += (float)c[j] * w; w *= q; if (run < left) bin = bin0 + j + 1; }
+        s_int[0] = min(bin, FINE - 1);
       }
       __syncthreads();
       mine.bin = s_int[0];
-      told = told_all[1];
+      told = told_all[3];
       tell(mine);
-      last_bin = 0;
+      last_bin = -1;
 #pragma unroll
       for (int c = 0; c < CL; ++c) last_bin = max(last_bin, told[c].bin);
+      if (last_bin < 0) last_bin = FINE - 1;   // (not reached: whatever is above the first bound)
     }
     if (tid == 0) s_int[1] = 0;
     __syncthreads();
-    each_vec([&](int v, const float* x) {
+    if (listed) {
+      const float from = fmaxf(bound, W.least);
+#pragma unroll 4
+      for (int v = tid; v < vecs; v += NT) {
+        alignas(16) T e[VN];
+        vec(v, e);
+        if (!(largest(e) >= from)) continue;
         unsigned hits = 0;
 #pragma unroll
         for (int c = 0; c < VN; ++c) {
-          const bool on = x[c] > -INFINITY && W.eligible(x[c]);
-          if (!listed) { if (on) sum += W(x[c]); }
-          else if (on && x[c] >= bound && (fine == 0.f || x[c] == mx || min(FINE - 1, (int)((mx - x[c]) * fine)) <= last_bin)) hits |= 1u << c;
+          const float x = to_f32(e[c]);
+          if (x >= from && (fine == 0.f || x == mx || min(FINE - 1, (int)((mx - x) * fine)) <= last_bin)) hits |= 1u << c;
         }
-        if (listed && __any_sync(0xffffffffu, hits != 0)) {
-          const int cnt = __popc(hits);
-          int at = cnt;
-#pragma unroll
-          for (int o = 1; o < 32; o <<= 1) { const int y = __shfl_up_sync(0xffffffffu, at, o); if (lane >= o) at += y; }
-          int from = 0;
-          if (lane == 31) from = atomicAdd(s_int + 1, at);
-          at += __shfl_sync(0xffffffffu, from, 31) - cnt;
-#pragma unroll
-          for (int c = 0; c < VN; ++c)
-            if ((hits >> c) & 1u) { if (at < P.list) list[at] = full_key(ordered(x[c]), lo + v * VN + c - sh); ++at; }
+        if (!hits) continue;
+        int at = atomicAdd(s_int + 1, __popc(hits));
+#pragma unroll 1
+        for (; hits; hits &= hits - 1) {
+          const int c = v * VN + __ffs(hits) - 1;
+          if (at < P.list) list[at] = full_key(ordered(to_f32(STAGED ? xs[c] : base[c]) + 0.f), lo + c - sh);
+          ++at;
         }
-      });
-    u64 wsum = sum;                            // this warp's
+      }
+    } else {
+      for (int v = warp * wv + lane; v < v_end; v += 32) {
+        alignas(16) T e[VN];
+        vec(v, e);
+        if (!W.eligible(largest(e))) continue;
 #pragma unroll
-    for (int o = 16; o > 0; o >>= 1) wsum += __shfl_xor_sync(0xffffffffu, wsum, o);
+        for (int c = 0; c < VN; ++c) {
+          const float x = to_f32(e[c]);
+          if (W.eligible(x)) sum += W(x);
+        }
+      }
+    }
+    if (!listed) {
+      u64 wsum = sum;                          // this warp's
+#pragma unroll 1
+      for (int o = 16; o > 0; o >>= 1) wsum += __shfl_xor_sync(0xffffffffu, wsum, o);
+      mine.mass = block_sum(lane == 0 ? wsum : 0, red);
+      __syncthreads();
+      if (lane == 0) red[warp] = wsum;
+    }
     __syncthreads();
-    if (lane == 0) red[warp] = wsum;
-    __syncthreads();
-    mine.mass = 0;
-#pragma unroll
-    for (int w = 0; w < NW; ++w) mine.mass += red[w];
     mine.count = s_int[1];
-    told = told_all[2];
+    told = told_all[4];
     tell(mine);
     u64 mass_all = 0, mass_before = 0;
     int count = 0, at0 = 0;
@@ -403,35 +447,39 @@ __global__ void __launch_bounds__(SP_THREADS, 2) k_sample(const __grid_constant_
         int sw = NW - 1;
         u64 before = 0;
         bool found = false;
-#pragma unroll
+#pragma unroll 1
         for (int w = 0; w < NW; ++w) {
           const u64 next = run + red[w];
           if (!found && (double)next > goal) { sw = w; before = run; found = true; }
           run = next;
         }
+        // the segment's vectors, one a thread
         const int e_end = min(vecs, (sw + 1) * wv);
         if (tid == 0) s_int[0] = -1;
         for (int v0 = sw * wv; v0 < e_end; v0 += NT) {
-          float x[VN];
+          alignas(16) T e[VN];
           u64 w[VN], part = 0, all;
           const int v = v0 + tid;
-          if (v < e_end) vec(v, x);
+          if (v < e_end) vec(v, e);
 #pragma unroll
           for (int c = 0; c < VN; ++c) {
-            w[c] = v < e_end && x[c] > -INFINITY && W.eligible(x[c]) ? W(x[c]) : 0;
+            const float x = v < e_end ? to_f32(e[c]) : -INFINITY;
+            w[c] = W.eligible(x) ? W(x) : 0;
             part += w[c];
           }
-          u64 c0 = before + BlockOps<NT>::scan(part, red, all) - part;
+          u64 c0 = before + block_scan(part, red, &all) - part;
+          if (!((double)c0 > goal) && (double)(c0 + part) > goal) {
+            int at = -1;
 #pragma unroll
-          for (int c = 0; c < VN; ++c) {
-            if (!((double)c0 > goal) && (double)(c0 + w[c]) > goal) s_int[0] = lo + v * VN + c - sh;
-            c0 += w[c];
+            for (int c = 0; c < VN; ++c) { c0 += w[c]; if (at < 0 && (double)c0 > goal) at = c; }
+            s_int[0] = lo + v * VN + at - sh;
           }
           __syncthreads();
-          token = s_int[0];
-          if (token >= 0) break;
+          if (s_int[0] >= 0) break;
           before += all;
         }
+        __syncthreads();
+        token = s_int[0];
       }
     } else {
       if (!whole && CL > 1) {                  // the lists to the first CTA
@@ -446,12 +494,16 @@ __global__ void __launch_bounds__(SP_THREADS, 2) k_sample(const __grid_constant_
       if (rank > 0) return;
       u64 thr = 0;                             // kept: keys from here up
       // each(f): f(key) for every token in question, a key of 0 for none, the same number of calls in all threads of a warp
-      auto each_listed = [&](auto&& f) { for (int j0 = warp * 32; j0 < count; j0 += NT) f(j0 + lane < count ? list[j0 + lane] : 0ull); };
+      auto each_listed = [&](auto&& f) {
+#pragma unroll 4
+        for (int j0 = warp * 32; j0 < count; j0 += NT) f(j0 + lane < count ? list[j0 + lane] : 0ull);
+      };
       auto each_row = [&](auto&& f) {
+#pragma unroll 1
         for (int i0 = warp * 32; i0 < V; i0 += NT) {
           const int i = i0 + lane;
           const float x = i < V ? clean(to_f32(CL == 1 && STAGED ? xs[i + sh] : logits[i])) : -INFINITY;
-          f(x > -INFINITY && W.eligible(x) ? full_key(ordered(x), i) : 0ull);
+          f(W.eligible(x) ? full_key(ordered(x), i) : 0ull);
         }
       };
       auto score = [](u64 key) { return unordered((uint32_t)(key >> 32)); };
@@ -466,21 +518,21 @@ __global__ void __launch_bounds__(SP_THREADS, 2) k_sample(const __grid_constant_
         double target = mass ? (double)S.top_p * (double)mass_given : (double)S.top_k;
         for (bool top = true;; top = false) {
           auto bin_of = [&](uint32_t o) { const float x = unordered(o); return shift < 0 ? (x == mx ? 0 : min(NB - 1, (int)((mx - x) * fscale))) : (int)((kmax - o) >> shift); };
-          for (int b = tid; b < NB; b += NT) hist[b] = 0;
+          hist.clear();
           if (tid == 0) { s_int[0] = NB - 1; s_pick[0] = 0; }
           __syncthreads();
           each([&](u64 key) {
             const uint32_t o = (uint32_t)(key >> 32);
             if (key && o >= kmin && o <= kmax && key >= thr) {
               const u64 w = mass ? W(score(key)) : 1;
-              if (w) atomicAdd(hist + bin_of(o), w);
+              if (w) hist.add(bin_of(o), w);
             }
           });
           __syncthreads();
           u64 c[NB / NT], sum = 0, total;
 #pragma unroll
-          for (int j = 0; j < NB / NT; ++j) { c[j] = hist[tid * (NB / NT) + j]; sum += c[j]; }
-          u64 before = BlockOps<NT>::scan(sum, red, total) - sum;
+          for (int j = 0; j < NB / NT; ++j) { c[j] = hist.at(tid * (NB / NT) + j); sum += c[j]; }
+          u64 before = block_scan(sum, red, &total) - sum;
           if (top && mass && !mass_given) target = (double)S.top_p * (double)total;
           if (top && !mass && (double)total <= target) return;   // no more than that: all stay
 #pragma unroll
@@ -493,7 +545,7 @@ __global__ void __launch_bounds__(SP_THREADS, 2) k_sample(const __grid_constant_
           const int bin = s_int[0];
           base += s_pick[0];
           uint32_t omin = 0xffffffffu, omax = 0u;
-          u64* few = hist;                       // (the histogram has been read)
+          u64* few = reinterpret_cast<u64*>(hist.lo);                       // (the histogram has been read)
           each([&](u64 key) {
             const uint32_t o = (uint32_t)(key >> 32);
             if (key && o >= kmin && o <= kmax && key >= thr && bin_of(o) == bin) {
@@ -558,19 +610,19 @@ __global__ void __launch_bounds__(SP_THREADS, 2) k_sample(const __grid_constant_
       auto drawn = [&](auto&& each) {
         int shift = 0;
         while (((V - 1) >> shift) >= NB) ++shift;
-        for (int b = tid; b < NB; b += NT) hist[b] = 0;
+        hist.clear();
         __syncthreads();
         each([&](u64 key) {
           if (key && key >= thr) {
             const u64 w = W(score(key));
-            if (w) atomicAdd(hist + (~(uint32_t)key >> shift), w);
+            if (w) hist.add((int)(~(uint32_t)key >> shift), w);
           }
         });
         __syncthreads();
         u64 c[NB / NT], sum = 0, total;
 #pragma unroll
-        for (int j = 0; j < NB / NT; ++j) { c[j] = hist[tid * (NB / NT) + j]; sum += c[j]; }
-        u64 before = BlockOps<NT>::scan(sum, red, total) - sum;
+        for (int j = 0; j < NB / NT; ++j) { c[j] = hist.at(tid * (NB / NT) + j); sum += c[j]; }
+        u64 before = block_scan(sum, red, &total) - sum;
         const double goal = (double)u * (double)total;
 #pragma unroll
         for (int j = 0; j < NB / NT; ++j) {
@@ -581,17 +633,19 @@ __global__ void __launch_bounds__(SP_THREADS, 2) k_sample(const __grid_constant_
         __syncthreads();
         const int bin = s_int[0];
         const u64 base = s_pick[0];
-        u64* few = hist;                         // (at most vocab / NB <= NB tokens)
+        u64* few = reinterpret_cast<u64*>(hist.lo);                         // (at most vocab / NB <= NB tokens)
         each([&](u64 key) {
           if (key && key >= thr && (int)(~(uint32_t)key >> shift) == bin) few[atomicAdd(s_int + 1, 1)] = key;
         });
         __syncthreads();
         const int nb = s_int[1];
+        for (int a = tid; a < nb; a += NT) list[a] = W(score(few[a]));   // (the list is not needed any more)
+        __syncthreads();
         for (int a = tid; a < nb; a += NT) {
           const uint32_t idx = ~(uint32_t)few[a];
-          const u64 w = W(score(few[a]));
+          const u64 w = list[a];
           u64 run = base;
-          for (int j = 0; j < nb; ++j) if (~(uint32_t)few[j] < idx) run += W(score(few[j]));
+          for (int j = 0; j < nb; ++j) if (~(uint32_t)few[j] < idx) run += list[j];
           if (!((double)run > goal) && (double)(run + w) > goal) s_int[2] = (int)idx;
         }
         __syncthreads();
@@ -662,8 +716,8 @@ constexpr size_t SP_ROOM = 112 * 1024, SP_MOST = 227 * 1024 - 4096;
 template <typename T, int CL, bool STAGED> int launch_rows(SampleParams& P, cudaStream_t st) {
   auto kern = k_sample<T, CL, STAGED>;
   // the list takes what is left: of half an SM, or of a whole one where the slice needs more
-  const size_t least = sp_smem<T>(P.vocab, CL, STAGED, FINE / 2), room = least <= SP_ROOM ? SP_ROOM : SP_MOST;
-  P.list = FINE / 2 + (int)((room - least) / 8);
+  const size_t least = sp_smem<T>(P.vocab, CL, STAGED, LEAST_LIST), room = least <= SP_ROOM ? SP_ROOM : SP_MOST;
+  P.list = LEAST_LIST + (int)((room - least) / 8);
   const size_t smem = sp_smem<T>(P.vocab, CL, STAGED, P.list);
   SCK(cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)SP_MOST));
   cudaLaunchConfig_t cfg{};
@@ -679,8 +733,8 @@ template <typename T, int CL, bool STAGED> int launch_rows(SampleParams& P, cuda
 // CTAs a row: as many as keep two CTAs on every SM while the rows are few, and as the slices need to fit.
 template <typename T> int launch_sample(SampleParams& P, cudaStream_t st) {
   int cl = 1;
-  while (cl < 8 && (P.n_rows * cl * 2 <= 2 * 148 || sp_smem<T>(P.vocab, cl, true, FINE / 2) > SP_ROOM)) cl *= 2;
-  if (sp_smem<T>(P.vocab, cl, true, FINE / 2) > SP_MOST) return launch_rows<T, 8, false>(P, st);
+  while (cl < 8 && (P.n_rows * cl * 2 <= 2 * 148 || sp_smem<T>(P.vocab, cl, true, LEAST_LIST) > SP_ROOM)) cl *= 2;
+  if (sp_smem<T>(P.vocab, cl, true, LEAST_LIST) > SP_MOST) return launch_rows<T, 8, false>(P, st);
   switch (cl) {
     case 1: return launch_rows<T, 1, true>(P, st);
     case 2: return launch_rows<T, 2, true>(P, st);
