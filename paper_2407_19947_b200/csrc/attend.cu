@@ -4,7 +4,6 @@
 //
 // with the running maximum and sum of a softmax, so that K and V are read once.
 #include <algorithm>
-#include <cstdlib>
 #include <type_traits>
 
 #include "attend.cuh"
@@ -106,7 +105,9 @@ Form form_of(const stairs_paged* c, int n_heads, int n_req, int n_rows) {
   f.vectors = c->head_dim % v == 0 && c->page_stride % v == 0 && c->token_stride % v == 0 && c->head_stride % v == 0 && aligned16(c->k_dev) && aligned16(c->v_dev);
   f.ks = am_ks(c->head_dim);
   f.mg = am_groups(f.ks, n_rows, n_req, n_heads / c->n_kv_heads);
-  f.tc = f.vectors && c->dtype != DT_F32 && (long long)n_rows * (n_heads / c->n_kv_heads) > (getenv("ATT_TC_MIN") ? atoll(getenv("ATT_TC_MIN")) : 64ll) * n_req && tc_takes(c, 1.f);
+  // tcgen05 from more than one (wide heads) or two row groups on: four requests of 16384, heads of 128, 20 queries a key head: 87 us, split form 120;
+  // heads of 64, 17 queries 124 and 102, 33 queries 125 and 171
+  f.tc = f.vectors && c->dtype != DT_F32 && (long long)n_rows * (n_heads / c->n_kv_heads) > (f.ks >= 8 ? 16ll : 32ll) * n_req && tc_takes(c, 1.f);
   return f;
 }
 

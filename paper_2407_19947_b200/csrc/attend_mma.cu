@@ -419,7 +419,8 @@ __global__ void __launch_bounds__(MG * 128 + 64, am_ctas(KS, MG)) k_attend_mma(c
 template <typename T, int KS, int MG> int launch(const AttendParams& P, cudaStream_t st) {
   typedef Geo<KS, MG> G;
   auto kern = k_attend_mma<T, KS, MG>;
-  if (G::SMEM > 48 * 1024) SCK(cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, G::SMEM));
+  static std::atomic<unsigned long long> done{0};
+  if (int rc = allow_shared(done, reinterpret_cast<const void*>(kern), G::SMEM)) return rc;
   kern<<<am_grid(KS, MG), G::NT, G::SMEM, st>>>(P);
   SCK(cudaGetLastError());
   return launch_join<T, MG * 16>(P, am_grid(KS, MG), 4, st);

@@ -582,7 +582,8 @@ typedef CUresult (*EncodeFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void
 
 template <typename T, int HD> int launch(const TcParams& J, cudaStream_t st) {
   auto kern = k_attend_tc<T, HD>;
-  SCK(cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, at_smem<HD>()));
+  static std::atomic<unsigned long long> done{0};
+  if (int rc = allow_shared(done, reinterpret_cast<const void*>(kern), at_smem<HD>())) return rc;
   kern<<<AM_SMS, AT_THREADS, at_smem<HD>(), st>>>(J);
   SCK(cudaGetLastError());
   return launch_join<T, AT_ROWS, true>(J.a, AM_SMS, 8, st);

@@ -719,7 +719,8 @@ template <typename T, int CL, bool STAGED> int launch_rows(SampleParams& P, cuda
   const size_t least = sp_smem<T>(P.vocab, CL, STAGED, LEAST_LIST), room = least <= SP_ROOM ? SP_ROOM : SP_MOST;
   P.list = LEAST_LIST + (int)((room - least) / 8);
   const size_t smem = sp_smem<T>(P.vocab, CL, STAGED, P.list);
-  SCK(cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)SP_MOST));
+  static std::atomic<unsigned long long> done{0};
+  if (int rc = allow_shared(done, reinterpret_cast<const void*>(kern), (int)SP_MOST)) return rc;
   cudaLaunchConfig_t cfg{};
   cfg.gridDim = dim3(P.n_rows * CL); cfg.blockDim = dim3(SP_THREADS); cfg.dynamicSmemBytes = smem; cfg.stream = st;
   cudaLaunchAttribute at[1];

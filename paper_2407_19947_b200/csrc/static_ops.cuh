@@ -1,5 +1,7 @@
 // What the entry points on caller-held buffers (paged.cu, attend.cu, sample.cu) share.
 #pragma once
+#include <atomic>
+
 #include "../../include/stairs.h"
 #include "common.cuh"
 
@@ -15,6 +17,17 @@ int static_fail(int code, const char* fmt, ...);
       return stairs::static_fail(STAIRS_ECUDA, "%s failed: %s (%s:%d)", #call, cudaGetErrorString(e_),  \
                                  __FILE__, __LINE__);                                                   \
   } while (0)
+
+// Lets `kern` have `bytes` of shared memory, once per device (the call takes the host about a microsecond).
+inline int allow_shared(std::atomic<unsigned long long>& done, const void* kern, int bytes) {
+  int dev = 0;
+  SCK(cudaGetDevice(&dev));
+  const unsigned long long bit = 1ull << (dev & 63);
+  if (dev < 64 && (done.load(std::memory_order_relaxed) & bit)) return STAIRS_OK;
+  SCK(cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes));
+  if (dev < 64) done.fetch_or(bit, std::memory_order_relaxed);
+  return STAIRS_OK;
+}
 
 enum Dtype { DT_F32 = 0, DT_BF16 = 1, DT_F16 = 2 };
 inline int dtype_bytes(int dt) { return dt == DT_F32 ? 4 : 2; }

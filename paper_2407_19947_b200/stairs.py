@@ -10,6 +10,7 @@ import collections
 import ctypes as C
 import functools
 import os
+import struct
 from typing import List, Optional, Sequence
 
 import numpy as np
@@ -111,12 +112,12 @@ def load_library(path: Optional[str] = None):
     lib.stairs_destroy.argtypes = [vp]
     lib.stairs_accept_static.argtypes = [vp, C.c_int, C.c_int, C.c_int, i32p, vp, C.c_int, vp, vp, vp]
     lib.stairs_tables_static.argtypes = [C.c_int, vp, vp, vp, vp, C.c_int, C.c_int, vp, C.c_int, vp, C.c_int] + [vp] * 9
-    lib.stairs_append_static.argtypes = [C.POINTER(CPaged), C.c_int, vp, vp, C.c_int, C.c_int64, C.c_int64, vp, vp]
+    lib.stairs_append_static.argtypes = [vp, C.c_int, vp, vp, C.c_int, C.c_int64, C.c_int64, vp, vp]
     lib.stairs_attend_workspace_bytes.restype = C.c_size_t
     lib.stairs_attend_workspace_bytes.argtypes = [C.POINTER(CPaged), C.c_int, C.c_int, C.c_int]
-    lib.stairs_attend_static.argtypes = [C.POINTER(CPaged), vp, C.c_int, C.c_int, vp, vp, C.c_int, C.c_int, C.c_int, vp, C.c_int64,
+    lib.stairs_attend_static.argtypes = [vp, vp, C.c_int, C.c_int, vp, vp, C.c_int, C.c_int, C.c_int, vp, C.c_int64,
                                          C.c_int64, C.c_float, vp, C.c_int64, C.c_int64, vp, C.c_size_t, vp]
-    lib.stairs_sample_static.argtypes = [vp, C.c_int, C.c_int, C.c_int64, C.c_int, i32p, C.POINTER(CSampling), vp, vp, C.c_int, vp, vp, vp]
+    lib.stairs_sample_static.argtypes = [vp, C.c_int, C.c_int, C.c_int64, C.c_int, i32p, vp, vp, vp, C.c_int, vp, vp, vp]
     lib.stairs_last_error.restype = C.c_char_p
     lib.stairs_last_error.argtypes = [vp]
     for name in EXPORTS:
@@ -364,33 +365,51 @@ def accept_static(logits_dev, k: Sequence[int], draft_dev, k_max: int, *, vocab:
 
 
 # -- the other steps of a pass on caller-held buffers (include/stairs.h) -----------------------------------------------
-# All tensors of a call lie on one CUDA device; the work is enqueued on `stream` (keyword), or on that device's current stream.
+# All tensors of a call lie on one CUDA device; the work is enqueued on `stream` (keyword), or on that device's current stream.  Small calls
+# are bound by this file's share of the time, hence checks in plain comparisons and structures packed by hand.
 Tables = collections.namedtuple("Tables", "n_blocks n_used row_off kv_len row_req row_pos row_slot n_served")
+
+_torch = None
+_DTYPES = {}                       # torch dtype -> the library's number
+_PAGED = struct.Struct("@PPqqqiiiii4x")
+_SAMPLING = struct.Struct("@fiff")
+
+
+def _t():
+    global _torch
+    if _torch is None:
+        import torch
+        _DTYPES.update({torch.float32: 0, torch.bfloat16: 1, torch.float16: 2})
+        _torch = torch
+    return _torch
 
 
 def _dtype_code(t):
-    code = {"torch.float32": 0, "torch.bfloat16": 1, "torch.float16": 2}.get(str(t.dtype))
+    _t()
+    code = _DTYPES.get(t.dtype)
     if code is None:
         raise ValueError(f"stairs: tensors of {t.dtype} are not supported (float32, bfloat16, float16)")
     return code
 
 
-def _need(ok, text):
-    if not ok:
-        raise ValueError("stairs: " + text)
+def _refuse(text):
+    raise ValueError("stairs: " + text)
 
 
-def _on_device(torch, first, *others):
-    """Device index of the tensors of a call; they have to share it."""
-    _need(first.is_cuda, "tensors have to be on a CUDA device")
-    dev = first.get_device()
-    for t in others:
-        _need(t is None or t.get_device() == dev, "tensors of one call have to be on one device")
+def _device_of(*tensors):
+    """Device index of the tensors of a call, which have to share a CUDA device."""
+    dev = tensors[0].get_device()
+    if dev < 0:
+        _refuse("tensors have to be on a CUDA device")
+    for t in tensors:
+        if t is not None and t.get_device() != dev:
+            _refuse("tensors of one call have to be on one device")
     return dev
 
 
-def _ints_1d(torch, t, n, name):
-    _need(t.dtype == torch.int32 and t.is_contiguous() and t.numel() == n, f"{name} has to be {n} contiguous int32 numbers")
+def _ints_1d(t, n, name):
+    if t.dtype != _torch.int32 or t.numel() != n or not t.is_contiguous():
+        _refuse(f"{name} has to be {n} contiguous int32 numbers")
 
 
 def _on_stream(f):
@@ -399,31 +418,32 @@ def _on_stream(f):
     def g(*a, stream=None, **kw):
         if stream is None:
             return f(*a, **kw)
-        import torch
-        with torch.cuda.stream(stream):
+        with _t().cuda.stream(stream):
             return f(*a, **kw)
     return g
 
 
-def _run(torch, dev, call):
-    """call(raw stream) with the tensors' device current; raises what the library refuses."""
-    st = torch._C._cuda_getCurrentRawStream(dev)
-    if torch._C._cuda_getDevice() == dev:
-        rc = call(st)
+def _call(dev, fn, *args):
+    """fn(*args, the device's current raw stream) with that device current; raises what the library refuses."""
+    c = _torch._C
+    if c._cuda_getDevice() == dev:
+        rc = fn(*args, c._cuda_getCurrentRawStream(dev))
     else:
-        with torch.cuda.device(dev):
-            rc = call(st)
+        with _torch.cuda.device(dev):
+            rc = fn(*args, c._cuda_getCurrentRawStream(dev))
     if rc:
-        raise StairsError(rc, load_library().stairs_last_error(None).decode())
+        raise StairsError(rc, _lib.stairs_last_error(None).decode())
 
 
-def _paged(torch, k_cache, v_cache):
-    _need(k_cache.dim() == 4 and k_cache.shape == v_cache.shape and k_cache.dtype == v_cache.dtype and k_cache.stride() == v_cache.stride(),
-          "k_cache and v_cache have to be alike: [pages, page_tokens, kv_heads, head_dim] of one type, with the same strides")
-    n, p, h, d = k_cache.shape
-    s = k_cache.stride()
-    _need(d == 1 or s[3] == 1, "a head's elements have to be next to each other in the cache")
-    return CPaged(k_cache.data_ptr(), v_cache.data_ptr(), s[0], s[1], s[2], n, p, h, d, _dtype_code(k_cache))
+def _paged(k_cache, v_cache):
+    """(a stairs_paged as bytes, kv_heads, head_dim)"""
+    code, shape, st = _dtype_code(k_cache), k_cache.shape, k_cache.stride()
+    if len(shape) != 4 or v_cache.shape != shape or v_cache.dtype != k_cache.dtype or v_cache.stride() != st:
+        _refuse("k_cache and v_cache have to be alike: [pages, page_tokens, kv_heads, head_dim] of one type, with the same strides")
+    n, p, h, d = shape
+    if d != 1 and st[3] != 1:
+        _refuse("a head's elements have to be next to each other in the cache")
+    return _PAGED.pack(k_cache.data_ptr(), v_cache.data_ptr(), st[0], st[1], st[2], n, p, h, d, code), h, d
 
 
 @_on_stream
@@ -431,86 +451,100 @@ def tables_static(n_seq, n_new, n_blocks, block_table, free_pages, n_used, *, pa
     """stairs_tables_static: block tables and row maps of the next pass from the requests' lengths, all on the device.
     n_seq, n_new, n_blocks: int32 [n_req]; block_table: int32 [n_req, max_blocks], completed in place; free_pages: int32
     [n_free], of which the first n_used (int32 [1]) are taken.  Returns the new counts and the maps of max_rows rows."""
-    import torch
-    lib = load_library()
+    torch, lib = _t(), load_library()
     n = n_seq.numel()
-    dev = _on_device(torch, n_seq, n_new, n_blocks, block_table, free_pages, n_used)
-    _ints_1d(torch, n_seq, n, "n_seq")
-    _ints_1d(torch, n_new, n, "n_new")
-    _ints_1d(torch, n_blocks, n, "n_blocks")
-    _ints_1d(torch, n_used, 1, "n_used")
-    _ints_1d(torch, free_pages, free_pages.numel(), "free_pages")
-    _need(block_table.dim() == 2 and block_table.shape[0] == n, "block_table has to be [n_req, max_blocks]")
-    _ints_1d(torch, block_table, block_table.numel(), "block_table")
-    _need(max_rows >= 0, "max_rows is negative")
-    device = n_seq.device
-    out = torch.empty(3 * n + 3 + 2 * max_rows, dtype=torch.int32, device=device)
-    slot = torch.empty(max_rows, dtype=torch.int64, device=device)
-    n_blocks_out, n_used_out, row_off, kv_len, row_req, row_pos, n_served = out.split([n, 1, n + 1, n, max_rows, max_rows, 1])
+    dev = _device_of(n_seq, n_new, n_blocks, block_table, free_pages, n_used)
+    _ints_1d(n_seq, n, "n_seq")
+    _ints_1d(n_new, n, "n_new")
+    _ints_1d(n_blocks, n, "n_blocks")
+    _ints_1d(n_used, 1, "n_used")
+    n_free = free_pages.numel()
+    _ints_1d(free_pages, n_free, "free_pages")
+    shape = block_table.shape
+    if len(shape) != 2 or shape[0] != n:
+        _refuse("block_table has to be [n_req, max_blocks]")
+    _ints_1d(block_table, n * shape[1], "block_table")
+    if max_rows < 0:
+        _refuse("max_rows is negative")
+    out = n_seq.new_empty(3 * n + 3 + 2 * max_rows)
+    slot = n_seq.new_empty(max_rows, dtype=torch.int64)
     at = out.data_ptr()
-    off = [at, at + 4 * n, at + 4 * (n + 1), at + 4 * (2 * n + 2), at + 4 * (3 * n + 2), at + 4 * (3 * n + 2 + max_rows)]
-    _run(torch, dev, lambda st: lib.stairs_tables_static(
-        n, n_seq.data_ptr(), n_new.data_ptr(), n_blocks.data_ptr(), block_table.data_ptr(), block_table.shape[1], page_tokens, free_pages.data_ptr(),
-        free_pages.numel(), n_used.data_ptr(), max_rows, *off, slot.data_ptr(), at + 4 * (3 * n + 2 + 2 * max_rows), st))
-    return Tables(n_blocks_out, n_used_out, row_off, kv_len, row_req, row_pos, slot, n_served)
+    rows = at + 4 * (3 * n + 2)
+    _call(dev, lib.stairs_tables_static, n, n_seq.data_ptr(), n_new.data_ptr(), n_blocks.data_ptr(), block_table.data_ptr(), shape[1], page_tokens,
+          free_pages.data_ptr(), n_free, n_used.data_ptr(), max_rows, at, at + 4 * n, at + 4 * n + 4, at + 8 * n + 8, rows, rows + 4 * max_rows, slot.data_ptr(),
+          rows + 8 * max_rows)
+    b, used, off, kv, req, pos, served = torch.split_with_sizes(out, (n, 1, n + 1, n, max_rows, max_rows, 1))
+    return Tables(b, used, off, kv, req, pos, slot, served)
 
 
 @_on_stream
 def append_static(k_new, v_new, k_cache, v_cache, row_slot) -> None:
     """stairs_append_static: rows of new keys and values ([rows, kv_heads, head_dim]) to their slots of the cache
     ([pages, page_tokens, kv_heads, head_dim], any strides).  row_slot: int64 [rows], negative for none."""
-    import torch
-    lib = load_library()
-    dev = _on_device(torch, k_new, v_new, k_cache, v_cache, row_slot)
-    c = _paged(torch, k_cache, v_cache)
-    _need(k_new.dim() == 3 and k_new.shape == v_new.shape and k_new.dtype == v_new.dtype and k_new.stride() == v_new.stride(),
-          "k_new and v_new have to be alike: [rows, kv_heads, head_dim] of one type, with the same strides")
-    rows, h, d = k_new.shape
-    s = k_new.stride()
-    _need(h == c.n_kv_heads and d == c.head_dim and (d == 1 or s[2] == 1), "k_new does not fit the cache")
-    _need(row_slot.dtype == torch.int64 and row_slot.is_contiguous() and row_slot.numel() == rows, "row_slot has to be one int64 number a row")
-    code = _dtype_code(k_new)
-    _run(torch, dev, lambda st: lib.stairs_append_static(C.byref(c), rows, k_new.data_ptr(), v_new.data_ptr(), code, s[0], s[1],
-                                                                 row_slot.data_ptr(), st))
+    torch, lib = _t(), load_library()
+    dev = _device_of(k_new, v_new, k_cache, v_cache, row_slot)
+    c, heads, hd = _paged(k_cache, v_cache)
+    shape, st = k_new.shape, k_new.stride()
+    if len(shape) != 3 or v_new.shape != shape or v_new.dtype != k_new.dtype or v_new.stride() != st:
+        _refuse("k_new and v_new have to be alike: [rows, kv_heads, head_dim] of one type, with the same strides")
+    rows, h, d = shape
+    if h != heads or d != hd or (d != 1 and st[2] != 1):
+        _refuse("k_new does not fit the cache")
+    if row_slot.dtype != torch.int64 or row_slot.numel() != rows or not row_slot.is_contiguous():
+        _refuse("row_slot has to be one int64 number a row")
+    _call(dev, lib.stairs_append_static, c, rows, k_new.data_ptr(), v_new.data_ptr(), _dtype_code(k_new), st[0], st[1], row_slot.data_ptr())
+
+
+@functools.lru_cache(maxsize=1024)
+def _attend_scratch(page_tokens, kv_heads, head_dim, code, heads, n_req, rows):
+    """Bytes that a call of these sizes asks for (a cache of any length and strides)."""
+    c = CPaged(4096, 4096, 4096, 4096, 4096, 2, page_tokens, kv_heads, head_dim, code)   # (addresses and strides that every form of the kernels takes)
+    return load_library().stairs_attend_workspace_bytes(C.byref(c), heads, n_req, rows)
 
 
 @_on_stream
 def attend_static(q, k_cache, v_cache, block_table, row_off, kv_len, *, scale: Optional[float] = None, max_len: int = 0, out=None):
     """stairs_attend_static: attention of the new rows' queries [rows, heads, head_dim] over the paged cache.  block_table: int32
     [n_req, max_blocks]; row_off: int32 [n_req + 1]; kv_len: int32 [n_req], the new rows included; scale: 1 / sqrt(head_dim) if None;
-    max_len: bound of kv_len (0: what the table can hold), which helps to divide the work.  Returns `out`, by default a new
-    tensor; rows of no request are not written."""
-    import torch
-    lib = load_library()
-    dev = _on_device(torch, q, k_cache, v_cache, block_table, row_off, kv_len, out)
-    c = _paged(torch, k_cache, v_cache)
+    max_len: bound of kv_len (0: what the table can hold).  Returns `out`, by default a new tensor; rows of no request are not written."""
+    torch, lib = _t(), load_library()
+    dev = _device_of(q, k_cache, v_cache, block_table, row_off, kv_len, out)
+    c, kv_heads, hd = _paged(k_cache, v_cache)
     n = kv_len.numel()
-    _need(q.dim() == 3 and q.dtype == k_cache.dtype and q.shape[2] == c.head_dim and (c.head_dim == 1 or q.stride(2) == 1),
-          "q has to be [rows, heads, head_dim] of the cache's type, a head's elements next to each other")
-    _ints_1d(torch, row_off, n + 1, "row_off")
-    _ints_1d(torch, kv_len, n, "kv_len")
-    _need(block_table.dim() == 2 and block_table.shape[0] == n, "block_table has to be [n_req, max_blocks]")
-    _ints_1d(torch, block_table, block_table.numel(), "block_table")
-    rows, heads, hd = q.shape
+    shape, st = q.shape, q.stride()
+    if len(shape) != 3 or q.dtype != k_cache.dtype or shape[2] != hd or (hd != 1 and st[2] != 1):
+        _refuse("q has to be [rows, heads, head_dim] of the cache's type, a head's elements next to each other")
+    _ints_1d(row_off, n + 1, "row_off")
+    _ints_1d(kv_len, n, "kv_len")
+    bt = block_table.shape
+    if len(bt) != 2 or bt[0] != n:
+        _refuse("block_table has to be [n_req, max_blocks]")
+    _ints_1d(block_table, n * bt[1], "block_table")
+    rows, heads, _ = shape
     if out is None:
-        out = torch.empty((rows, heads, hd), dtype=q.dtype, device=q.device)
-    else:
-        _need(out.shape == q.shape and out.dtype == q.dtype and (hd == 1 or out.stride(2) == 1), "out has to be like q")
-    need = lib.stairs_attend_workspace_bytes(C.byref(c), heads, n, rows)
-    ws = torch.empty(need, dtype=torch.uint8, device=q.device) if need else None
-    _run(torch, dev, lambda st: lib.stairs_attend_static(
-        C.byref(c), block_table.data_ptr(), block_table.shape[1], n, row_off.data_ptr(), kv_len.data_ptr(), max_len, rows, heads, q.data_ptr(),
-        q.stride(0), q.stride(1), hd ** -0.5 if scale is None else scale, out.data_ptr(), out.stride(0), out.stride(1),
-        ws.data_ptr() if need else None, need, st))
+        out = q.new_empty(shape)
+    elif out.shape != shape or out.dtype != q.dtype or (hd != 1 and out.stride(2) != 1):
+        _refuse("out has to be like q")
+    need = _attend_scratch(k_cache.shape[1], kv_heads, hd, _DTYPES[q.dtype], heads, n, rows) if rows else 0
+    ws = q.new_empty(need, dtype=torch.uint8) if need else None
+    so = out.stride()
+    _call(dev, lib.stairs_attend_static, c, block_table.data_ptr(), bt[1], n, row_off.data_ptr(), kv_len.data_ptr(), max_len, rows, heads, q.data_ptr(),
+          st[0], st[1], hd ** -0.5 if scale is None else scale, out.data_ptr(), so[0], so[1], ws.data_ptr() if need else None, need)
     return out
 
 
 def _settings(n, temperature, top_k, top_p, min_p):
-    """One CSampling per request; each setting is a number for all or a sequence."""
-    each = [[v] * n if isinstance(v, (int, float)) else v for v in (temperature, top_k, top_p, min_p)]
+    """n stairs_sampling as bytes; each setting is a number for all or a sequence."""
+    each = (temperature, top_k, top_p, min_p)
+    try:
+        return _SAMPLING.pack(*each) * n            # numbers
+    except struct.error:
+        pass
+    each = [[v] * n if isinstance(v, (int, float)) else v for v in each]
     for v, name in zip(each, ("temperature", "top_k", "top_p", "min_p")):
-        _need(len(v) == n, f"{name} has to be one number, or one for each of the {n} requests")
-    return (CSampling * n)(*zip(*each))
+        if len(v) != n:
+            _refuse(f"{name} has to be one number, or one for each of the {n} requests")
+    return struct.pack("@" + "fiff" * n, *[x for s in zip(*each) for x in s])
 
 
 @_on_stream
@@ -519,22 +553,30 @@ def sample_static(logits, k: Sequence[int], draft_dev, k_max: int, u, *, tempera
     """stairs_sample_static: accept_static with a token drawn for every row instead of the greedy one.  logits: [rows, ld] of
     float32, bfloat16 or float16; u: float32 [rows] random numbers in [0, 1); temperature, top_k, top_p and min_p: a number for all
     requests or one for each.  Returns (tokens [n_req, k_max + 1], accept_len [n_req])."""
-    import torch
-    lib = load_library()
+    torch, lib = _t(), load_library()
     kk = _ints(k)
     ks = kk[:]
-    n, rows = len(ks), sum(ks) + len(ks)
-    dev = _on_device(torch, logits, draft_dev, u)
-    _need(logits.dim() == 2 and logits.shape[0] >= rows and (logits.shape[1] == 1 or logits.stride(1) == 1), f"logits have to be [{rows}, vocab]")
-    _need(rows == 1 or logits.stride(0) >= logits.shape[1], "the logits' rows overlap")
-    _need(vocab is None or 0 < vocab <= logits.shape[1], "vocab is more than the logits have")
-    _need(u.dtype == torch.float32 and u.is_contiguous() and u.numel() >= rows, "u has to be one contiguous float32 number a row")
-    if draft_dev is not None:
-        _need(draft_dev.dtype == torch.int32 and draft_dev.is_contiguous() and draft_dev.numel() >= n * k_max, "draft_dev has to be int32 [n_req, k_max]")
-    code, s = _dtype_code(logits), _settings(n, temperature, top_k, top_p, min_p)
-    _need(0 <= k_max <= 63, "k_max outside 0..63")
-    tt, al = _results(torch, n, k_max, ks, logits.device)
-    _run(torch, dev, lambda st: lib.stairs_sample_static(
-        logits.data_ptr(), code, vocab or logits.shape[1], max(logits.stride(0), logits.shape[1]), n, kk, s, u.data_ptr(),
-        draft_dev.data_ptr() if draft_dev is not None else None, k_max, tt.data_ptr(), al.data_ptr(), st))
+    n = len(ks)
+    rows = sum(ks) + n
+    dev = _device_of(logits, draft_dev, u)
+    code, shape, st = _dtype_code(logits), logits.shape, logits.stride()
+    if len(shape) != 2 or shape[0] < rows or (shape[1] != 1 and st[1] != 1):
+        _refuse(f"logits have to be [{rows}, vocab]")
+    if rows != 1 and st[0] < shape[1]:
+        _refuse("the logits' rows overlap")
+    if vocab is not None and not 0 < vocab <= shape[1]:
+        _refuse("vocab is more than the logits have")
+    if u.dtype != torch.float32 or u.numel() < rows or not u.is_contiguous():
+        _refuse("u has to be one contiguous float32 number a row")
+    if not 0 <= k_max <= 63:
+        _refuse("k_max outside 0..63")
+    if draft_dev is not None and (draft_dev.dtype != torch.int32 or draft_dev.numel() < n * k_max or not draft_dev.is_contiguous()):
+        _refuse("draft_dev has to be int32 [n_req, k_max]")
+    s = _settings(n, temperature, top_k, top_p, min_p)
+    if min(ks, default=0) >= k_max:
+        tt, al = u.new_empty((n, k_max + 1), dtype=torch.int32), u.new_empty(n, dtype=torch.int32)
+    else:                                            # (entries past a request's own draft length are zero)
+        tt, al = u.new_zeros((n, k_max + 1), dtype=torch.int32), u.new_empty(n, dtype=torch.int32)
+    _call(dev, lib.stairs_sample_static, logits.data_ptr(), code, vocab or shape[1], max(st[0], shape[1]), n, kk, s, u.data_ptr(),
+          draft_dev.data_ptr() if draft_dev is not None else None, k_max, tt.data_ptr(), al.data_ptr())
     return tt, al

@@ -1,6 +1,7 @@
 """What the entry points on caller-held buffers refuse: checked on the host, before anything is enqueued, so no device is needed
 (the addresses below are never followed)."""
 import ctypes as C
+import struct
 
 import pytest
 
@@ -106,8 +107,25 @@ def test_binding_refuses_tensors_that_do_not_fit():
     with pytest.raises(ValueError, match="top_p"):
         st._settings(2, 1.0, 0, [0.5], 0.0)
     with pytest.raises(ValueError, match="alike"):
-        st._paged(torch, z(2, 4, 1, 8), z(2, 4, 1, 16))
+        st._paged(z(2, 4, 1, 8), z(2, 4, 1, 16))
     with pytest.raises(ValueError, match="next to each other"):
-        st._paged(torch, z(2, 4, 8, 3).transpose(2, 3), z(2, 4, 8, 3).transpose(2, 3))
+        st._paged(z(2, 4, 8, 3).transpose(2, 3), z(2, 4, 8, 3).transpose(2, 3))
     with pytest.raises(ValueError, match="not supported"):
         st._dtype_code(z(1, dtype=torch.float64))
+
+
+def test_binding_packs_the_structures_of_the_header():
+    # the hand-packed structures against the ctypes ones, field by field
+    import torch
+    k, v = torch.zeros(3, 16, 2, 8, dtype=torch.float16), torch.zeros(3, 16, 2, 8, dtype=torch.float16)
+    raw, heads, hd = st._paged(k.transpose(1, 2).contiguous().transpose(1, 2), v.transpose(1, 2).contiguous().transpose(1, 2))
+    c = st.CPaged.from_buffer_copy(raw)
+    assert (c.page_stride, c.token_stride, c.head_stride, c.n_pages, c.page_tokens, c.n_kv_heads, c.head_dim, c.dtype) == (256, 8, 128, 3, 16, 2, 8, 2)
+    assert (heads, hd) == (2, 8)
+    one = (st.CSampling * 3).from_buffer_copy(st._settings(3, 0.5, 7, 0.25, 0.125))
+    many = (st.CSampling * 3).from_buffer_copy(st._settings(3, [0.5, 1.0, 2], 7, [0.25] * 3, 0.125))
+    assert [(s.temperature, s.top_k, s.top_p, s.min_p) for s in one] == [(0.5, 7, 0.25, 0.125)] * 3
+    assert [(s.temperature, s.top_k, s.top_p, s.min_p) for s in many] == [(0.5, 7, 0.25, 0.125), (1.0, 7, 0.25, 0.125), (2.0, 7, 0.25, 0.125)]
+    for bad in ([1], 1.5, "x", 2**31):
+        with pytest.raises((ValueError, TypeError, struct.error)):
+            st._settings(3, 1.0, bad, 1.0, 0.0)
