@@ -16,7 +16,8 @@ namespace att {
 namespace {
 
 __device__ __forceinline__ void cp16(uint32_t dst, const void* src, bool on) {   // zeros where off
-  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(on ? 16 : 0) : "memory");
+  // (no memory clobber: a step's addresses are read before its copies are asked for, not one behind another; the barriers around them order the rest)
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(on ? 16 : 0));
 }
 __device__ __forceinline__ void cp_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 template <int N> __device__ __forceinline__ void cp_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
@@ -91,45 +92,70 @@ __global__ void __launch_bounds__(MG * 128 + 64, am_ctas(KS, MG)) k_attend_mma(c
     total = all;
     return v + before;
   };
-  long long total = 0, mine_incl = 0, mine = 0;
-  for (int base = 0; base < P.n_req; base += G::NT) {
-    int chunks;
-    mine = base + tid < P.n_req ? steps_of(request_span(P, base + tid), chunks) : 0;
-    long long all;
-    mine_incl = scan(mine, all) + total;
-    total += all;
-  }
-  const long long parts_all = min((long long)gridDim.x, total);    // CTAs with a part: each has a step at least
+  auto divide = [](long long a, long long b) { return ((a | b) >> 32) == 0 ? (long long)((unsigned)a / (unsigned)b) : a / b; };
+  long long total = 0, x0, x1, rem0, parts_all;   // parts_all: CTAs with a part (each has a step at least); rem0: this one's first step, within request req0
+  int req0;
+  Span span0;
   Meta* meta = reinterpret_cast<Meta*>(P.ws) + blockIdx.x;
-  if (blockIdx.x >= parts_all) {
-    if (tid == 0) meta->parts = 0;
-    return;
-  }
-  const long long x0 = total * blockIdx.x / parts_all, x1 = total * (blockIdx.x + 1) / parts_all;
-  if (P.n_req <= G::NT) {
-    if (x0 >= mine_incl - mine && x0 < mine_incl) { s_req = tid; s_rem = x0 - (mine_incl - mine); }
+  auto shares = [&]() {
+    parts_all = min((long long)gridDim.x, total);
+    x0 = x1 = 0;
+    if (blockIdx.x < parts_all) { x0 = divide(total * blockIdx.x, parts_all); x1 = divide(total * (blockIdx.x + 1), parts_all); }
+  };
+  if (P.n_req <= 32) {                             // every warp by itself
+    int chunks;
+    Span s{0, 0, 0};
+    if (lane < P.n_req) s = request_span(P, lane);
+    const long long v = lane < P.n_req ? steps_of(s, chunks) : 0;
+    long long incl = v;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const long long u = __shfl_up_sync(0xffffffffu, incl, o);
+      if (lane >= o) incl += u;
+    }
+    total = __shfl_sync(0xffffffffu, incl, 31);
+    shares();
+    const unsigned here = __ballot_sync(0xffffffffu, x0 >= incl - v && x0 < incl);
+    req0 = here ? __ffs(here) - 1 : 0;
+    rem0 = x0 - __shfl_sync(0xffffffffu, incl - v, req0);
+    span0.first = __shfl_sync(0xffffffffu, s.first, req0); span0.n = __shfl_sync(0xffffffffu, s.n, req0); span0.len = __shfl_sync(0xffffffffu, s.len, req0);
   } else {
+    for (int base = 0; base < P.n_req; base += G::NT) {
+      int chunks;
+      long long all;
+      scan(base + tid < P.n_req ? steps_of(request_span(P, base + tid), chunks) : 0, all);
+      total += all;
+    }
+    shares();
     long long before = 0;
     for (int base = 0; base < P.n_req; base += G::NT) {
       int chunks;
       const long long v = base + tid < P.n_req ? steps_of(request_span(P, base + tid), chunks) : 0;
       long long all;
       const long long incl = scan(v, all) + before;
-      if (x0 >= incl - v && x0 < incl) { s_req = base + tid; s_rem = x0 - (incl - v); }
+      if (x1 > x0 && x0 >= incl - v && x0 < incl) { s_req = base + tid; s_rem = x0 - (incl - v); }
       before += all;
     }
+    __syncthreads();
+    if (x1 > x0) { req0 = s_req; rem0 = s_rem; span0 = request_span(P, req0); }
   }
-  __syncthreads();
+  if (x1 == x0) {
+    if (tid == 0) meta->parts = 0;
+    return;
+  }
   const int n_steps = (int)min(x1 - x0, 0x7fffffffll);
 
   const uint32_t sm0 = smem_addr(am_sm), q0 = smem_addr(qring);
   if (warp >= MG * 4) {
     // ---------------------------------------------------------------- two warps that walk the list and copy, one thread per position
     const int ct = tid - G::NC;
-    int req = s_req, chunks, unit, chunk;
-    Span sp = request_span(P, req);
-    int units = (int)(steps_of(sp, chunks) / chunks);
-    unit = (int)(s_rem / chunks); chunk = (int)(s_rem - (long long)unit * chunks);
+    int req = req0, chunks, unit, chunk;
+    Span sp = span0;
+    auto units_of = [&](const Span& s) { chunks = max(1, (s.len + AM_CHUNK - 1) / AM_CHUNK); return (int)(((long long)s.n * group + G::ROWS - 1) / G::ROWS) * P.kv_heads; };
+    int units = units_of(sp);
+    unit = (int)divide(rem0, chunks); chunk = (int)(rem0 - (long long)unit * chunks);
+    Meta end_meta{};
+    long long end_at = 0;                       // where the unit that goes on in the next CTAs ends
     int seg = 0, part_begin = chunk, planned = 0;
     Step plan;                                  // the step being planned, and this thread's position's place
     long long place = -1;
@@ -147,25 +173,16 @@ __global__ void __launch_bounds__(MG * 128 + 64, am_ctas(KS, MG)) k_attend_mma(c
         const int b = p / P.page_tokens, page = __ldg(P.table + (size_t)req * P.max_blocks + b);
         if (page >= 0 && page < P.n_pages) place = page * P.page_stride + (p - b * P.page_tokens) * P.token_stride;
       }
-      if (last && ct == 0) {
-        Meta m{};
-        if (plan.ends == 2 && part_begin == 0) {                       // the unit goes on in the next CTAs
-          // the CTA that holds the unit's last step: the first whose part ends behind it
-          const long long end = x1 + (chunks - 1 - chunk);             // one past the unit's last step
-          long long e = (end * parts_all - 1) / total;                 // (about; corrected below)
-          while (e > 0 && total * e / parts_all >= end) --e;
-          while (total * (e + 1) / parts_all < end) ++e;
-          m.parts = (int)(e - blockIdx.x) + 1;
-          m.slot = plan.slot; m.first = sp.first; m.n = sp.n; m.qb = plan.qb; m.h = plan.h;
-        }
-        *meta = m;
+      if (last && plan.ends == 2 && part_begin == 0) {
+        end_meta.slot = plan.slot; end_meta.first = sp.first; end_meta.n = sp.n; end_meta.qb = plan.qb; end_meta.h = plan.h;
+        end_at = x1 + (chunks - 1 - chunk);
       }
       if (unit_ends) {
         chunk = 0; ++seg; part_begin = 0;
         if (++unit == units && !last) {
           unit = 0;
           do { sp = request_span(P, ++req); } while (sp.n == 0);       // (there are steps left, so there is such a request)
-          units = (int)(steps_of(sp, chunks) / chunks);
+          units = units_of(sp);
         }
       } else ++chunk;
     };
@@ -192,14 +209,20 @@ __global__ void __launch_bounds__(MG * 128 + 64, am_ctas(KS, MG)) k_attend_mma(c
         const uint32_t dst = sm0 + (x % NST) * G::STAGE;
         const T* kb = reinterpret_cast<const T*>(P.kc) + s.h * P.head_stride;
         const T* vb = reinterpret_cast<const T*>(P.vc) + s.h * P.head_stride;
-#pragma unroll 8
-        for (int i = 0; i < G::PC; ++i) {
-          const int it = i * AM_CHUNK + ct, r = it / G::PC, c = it % G::PC;
-          const long long ro_r = ro[r];
-          const bool on = ro_r >= 0 && c < pieces;
-          const long long src = on ? ro_r + c * 8 : 0;
-          cp16(dst + G::at(r, c), kb + src, on);
-          cp16(dst + G::KV + G::at(r, c), vb + src, on);
+        constexpr int GRP = G::PC % 8 == 0 ? 8 : G::PC % 5 == 0 ? 5 : G::PC % 6 == 0 ? 6 : 4;   // addresses in registers at a time
+#pragma unroll 1
+        for (int i0 = 0; i0 < G::PC; i0 += GRP) {
+          long long at[GRP];
+#pragma unroll
+          for (int j = 0; j < GRP; ++j) at[j] = ro[((i0 + j) * AM_CHUNK + ct) / G::PC];
+#pragma unroll
+          for (int j = 0; j < GRP; ++j) {
+            const int it = (i0 + j) * AM_CHUNK + ct, r = it / G::PC, c = it % G::PC;
+            const bool on = at[j] >= 0 && c < pieces;
+            const long long src = on ? at[j] + c * 8 : 0;
+            cp16(dst + G::at(r, c), kb + src, on);
+            cp16(dst + G::KV + G::at(r, c), vb + src, on);
+          }
         }
         if (s.begins) {
           const uint32_t qd = q0 + (loaded_units % NST) * G::QB;
@@ -215,9 +238,14 @@ __global__ void __launch_bounds__(MG * 128 + 64, am_ctas(KS, MG)) k_attend_mma(c
       cp_commit();
     };
     auto copiers_sync = []() { asm volatile("bar.sync 2, 64;" ::: "memory"); };
-    for (int i = 0; i < NST; ++i) { plan_load(); plan_store(); }
-    copiers_sync();
-    for (int i = 0; i < NST - 1; ++i) issue(i);
+    for (int i = 0; i < NST - 1; ++i) {         // (copies of a step are on their way before the next one is planned)
+      plan_load();
+      plan_store();
+      copiers_sync();
+      issue(i);
+    }
+    plan_load();
+    plan_store();
     for (int x = 0; x < n_steps; ++x) {
       cp_wait<NST - 2>();
       __syncthreads();                          // step x has arrived; its predecessor's stage and entry are free
@@ -226,6 +254,16 @@ __global__ void __launch_bounds__(MG * 128 + 64, am_ctas(KS, MG)) k_attend_mma(c
       plan_store();
     }
     cp_wait<0>();
+    if (ct == 0) {
+      if (end_at) {
+        // the CTA that holds the unit's last step: the first whose part ends behind it
+        long long e = divide(end_at * parts_all - 1, total);           // (about; corrected below)
+        while (e > 0 && divide(total * e, parts_all) >= end_at) --e;
+        while (divide(total * (e + 1), parts_all) < end_at) ++e;
+        end_meta.parts = (int)(e - blockIdx.x) + 1;
+      }
+      *meta = end_meta;
+    }
     return;
   }
 
