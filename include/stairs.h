@@ -327,13 +327,17 @@ int stairs_append_static(const stairs_paged *cache, int n_rows, const void *k_ne
  * no request are left as they were.
  *   q_dev, o_dev      type of the cache; element (t, head, i) at t*row_stride + head*head_stride + i.
  *                     o_dev may not overlap the inputs
- *   max_len           bound of the requests' kv_len; 0: max_blocks * page_tokens
- *   workspace         stairs_attend_workspace_bytes(), 256-byte aligned: scratch of this call; calls
- *                     that may overlap on the GPU (and graphs that hold them) need one each
+ *   max_len           bound of the requests' kv_len; 0: max_blocks * page_tokens.  It decides with the
+ *                     other sizes how the work is divided: give the smallest that holds
+ *   workspace         stairs_attend_workspace_bytes() for the same sizes and max_len (0 there: for any),
+ *                     256-byte aligned, NULL where that is 0: scratch of this call; calls that may
+ *                     overlap on the GPU (and graphs that hold them) need one each
+ * A wait inside the kernel that runs out, which takes a broken device, leaves NaN in rows of the call.
  * Scores, softmax and sums are 32-bit; of 16-bit caches the softmax weights are rounded to 16 bits for
  * the product with V.  Limits: 1 <= n_req <= STAIRS_ATTEND_MAX_REQ, head_dim <= STAIRS_MAX_HEAD_DIM,
  * n_heads a multiple of n_kv_heads. */
-size_t stairs_attend_workspace_bytes(const stairs_paged *cache, int n_heads, int n_req, int n_rows);
+size_t stairs_attend_workspace_bytes(const stairs_paged *cache, int n_heads, int n_req, int n_rows,
+                                     int max_len);
 int stairs_attend_static(const stairs_paged *cache, const int32_t *block_table_dev, int max_blocks,
                          int n_req, const int32_t *row_off_dev, const int32_t *kv_len_dev, int max_len,
                          int n_rows, int n_heads, const void *q_dev, int64_t q_row_stride,

@@ -98,8 +98,8 @@ using namespace stairs;
 namespace {
 
 // The form that a call takes, by sizes and alignment alone (never by lengths, which the host does not know).
-struct Form { bool vectors, tc; int ks, mg; };
-Form form_of(const stairs_paged* c, int n_heads, int n_req, int n_rows) {
+struct Form { bool vectors, tc; int ks, mg, cluster; };
+Form form_of(const stairs_paged* c, int n_heads, int n_req, int n_rows, int max_len) {
   Form f{};
   const int v = 16 / dtype_bytes(c->dtype);
   f.vectors = c->head_dim % v == 0 && c->page_stride % v == 0 && c->token_stride % v == 0 && c->head_stride % v == 0 && aligned16(c->k_dev) && aligned16(c->v_dev);
@@ -107,18 +107,21 @@ Form form_of(const stairs_paged* c, int n_heads, int n_req, int n_rows) {
   f.mg = am_groups(f.ks, n_rows, n_req, n_heads / c->n_kv_heads);
   // tcgen05 from more than one (wide heads) or two row groups on: four requests of 16384, heads of 128, 20 queries a key head: 87 us, split form 120;
   // heads of 64, 17 queries 124 and 102, 33 queries 125 and 171
-  f.tc = f.vectors && c->dtype != DT_F32 && (long long)n_rows * (n_heads / c->n_kv_heads) > (f.ks >= 8 ? 16ll : 32ll) * n_req && tc_takes(c, 1.f);
+  f.cluster = am_cluster(f.ks, f.mg, n_rows, n_req, n_heads / c->n_kv_heads, c->n_kv_heads, max_len);
+  // (clusters where the call is small: one request of 2048, 20 queries a key head 21 us against 35)
+  f.tc = !f.cluster && f.vectors && c->dtype != DT_F32 && (long long)n_rows * (n_heads / c->n_kv_heads) > (f.ks >= 8 ? 16ll : 32ll) * n_req && tc_takes(c, 1.f);
   return f;
 }
 
 }  // namespace
 
-extern "C" size_t stairs_attend_workspace_bytes(const stairs_paged* cache, int n_heads, int n_req, int n_rows) {
+extern "C" size_t stairs_attend_workspace_bytes(const stairs_paged* cache, int n_heads, int n_req, int n_rows, int max_len) {
   if (check_paged("stairs_attend_workspace_bytes", cache)) return 0;
-  if (n_heads < 1 || n_heads % cache->n_kv_heads || n_req < 1 || n_rows < 1) return 0;
-  const Form f = form_of(cache, n_heads, n_req, n_rows);
+  if (n_heads < 1 || n_heads % cache->n_kv_heads || n_req < 1 || n_rows < 1 || max_len < 0) return 0;
+  const Form f = form_of(cache, n_heads, n_req, n_rows, max_len ? max_len : 0x7fffffff - AM_CHUNK);
   if (!f.vectors || cache->dtype == DT_F32) return 0;
-  const size_t mma = am_workspace(f.ks, f.mg, cache->head_dim);
+  // (a call that the tensor maps do not take - a scale of zero or less - goes the other way)
+  const size_t mma = f.cluster ? 0 : am_workspace(f.ks, f.mg, cache->head_dim);
   return f.tc ? std::max(mma, tc_workspace(cache->head_dim)) : mma;
 }
 
@@ -142,15 +145,16 @@ extern "C" int stairs_attend_static(const stairs_paged* cache, const int32_t* bl
   const int reach = max_blocks * cache->page_tokens;
   AttendParams P{cache->k_dev, cache->v_dev, q_dev, o_dev, cache->page_stride, cache->token_stride, cache->head_stride, q_row_stride, q_head_stride,
                  o_row_stride, o_head_stride, block_table_dev, row_off_dev, kv_len_dev, n_req, n_rows, n_heads, cache->n_kv_heads, cache->head_dim,
-                 cache->n_pages, cache->page_tokens, max_blocks, max_len ? std::min(max_len, reach) : reach, scale, workspace};
+                 cache->n_pages, cache->page_tokens, max_blocks, max_len ? std::min(max_len, reach) : reach, scale, workspace, 0};
   cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
-  const Form f = form_of(cache, n_heads, n_req, n_rows);
+  const Form f = form_of(cache, n_heads, n_req, n_rows, P.max_len);
   const int v = 16 / dtype_bytes(cache->dtype);
   if (f.vectors && cache->dtype != DT_F32 && aligned16(q_dev) && q_row_stride % v == 0 && q_head_stride % v == 0 && aligned16(o_dev) && o_row_stride % v == 0 &&
       o_head_stride % v == 0) {
     const bool tc = f.tc && scale > 0.f;
-    const size_t need = tc ? tc_workspace(cache->head_dim) : am_workspace(f.ks, f.mg, cache->head_dim);
-    if (!workspace || reinterpret_cast<uintptr_t>(workspace) % 256 || workspace_bytes < need)
+    P.cluster = tc ? 0 : f.cluster;
+    const size_t need = tc ? tc_workspace(cache->head_dim) : f.cluster ? 0 : am_workspace(f.ks, f.mg, cache->head_dim);
+    if (need && (!workspace || reinterpret_cast<uintptr_t>(workspace) % 256 || workspace_bytes < need))
       return static_fail(workspace && workspace_bytes < need ? STAIRS_ENOSPC : STAIRS_EINVAL, "%s: %zu bytes of scratch, 256-byte aligned, are needed; %zu at %p were given",
                          who, need, workspace_bytes, workspace);
     if (tc) return launch_tc(P, cache->dtype, st);

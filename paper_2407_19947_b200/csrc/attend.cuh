@@ -12,6 +12,7 @@ struct AttendParams {
   int n_req, n_rows, heads, kv_heads, hd, n_pages, page_tokens, max_blocks, max_len;
   float scale;
   void* ws;                     // caller's scratch
+  int cluster;                  // split form: CTAs that share a unit; 0: units cut evenly over all CTAs
 };
 
 __device__ __forceinline__ int clampi(int v, int lo, int hi) { return v < lo ? lo : (v > hi ? hi : v); }
@@ -31,7 +32,7 @@ constexpr int AM_CHUNK = 64;                   // positions per pipeline stage
 constexpr int AM_SMS = 148;
 constexpr int am_pitch(int ks) { return (ks * 2 % 8 == 0 ? ks * 2 : (ks * 2) | 1) * 16; }   // bytes of a staged row of ks 16-element steps
 constexpr int am_smem(int ks, int mg, int nst) {
-  return nst * (2 * AM_CHUNK + 16 * mg) * am_pitch(ks) + (nst + 1) * (AM_CHUNK * 8 + 48) + 8 * 16 * mg * 4 + 64;
+  return nst * (2 * AM_CHUNK + 16 * mg) * am_pitch(ks) + (nst + 1) * (AM_CHUNK * 8 + 64) + 10 * 16 * mg * 4 + 64;
 }
 // two CTAs share an SM where three stages and the registers of each fit, else one has as many stages as fit (at most six)
 constexpr int am_ctas(int ks, int mg) { return am_smem(ks, mg, 3) <= 112 * 1024 && (mg == 1 || (mg == 2 && ks <= 6)) ? 2 : 1; }
@@ -52,7 +53,18 @@ inline int am_ks(int hd) {
   for (int k : am_steps) if (hd <= 16 * k) return k;
   return 16;
 }
-inline size_t am_workspace(int ks, int mg, int hd) { return (size_t)am_grid(ks, mg) * (32 + (size_t)2 * 16 * mg * (hd + 2) * 4); }
+// Small calls: a cluster of CTAs for every unit, as many as keep the chip's SMs (those that clusters find free) busy and have a chunk
+// each, joined through distributed shared memory: one launch, no scratch.  0: too many units or too long for that (the lengths are
+// only known by their bound, and the longest request's CTAs would work alone at the end).
+inline int am_cluster(int ks, int mg, int n_rows, int n_req, int group, int kv_heads, int max_len) {
+  const long long q = (long long)n_rows * group, blocks = n_req == 1 ? (q + 16 * mg - 1) / (16 * mg) : q / (16 * mg) + n_req, units = blocks * kv_heads;
+  const int chunks = (max_len + AM_CHUNK - 1) / AM_CHUNK, room = 128 * am_ctas(ks, mg);
+  if (units > room) return 0;
+  int s = 1;
+  while (s < 8 && units * s * 2 <= room && s < chunks) s *= 2;
+  return (chunks + s - 1) / s <= 24 ? s : 0;
+}
+inline size_t am_workspace(int ks, int mg, int hd) { return (size_t)am_grid(ks, mg) * (64 + (size_t)2 * 16 * mg * (hd + 2) * 4) + 256; }
 template <int KS> int launch_mma(const AttendParams& P, int dtype, int mg, cudaStream_t st);   // KS: 16-element steps of a head
 
 // --- many queries per key head on tcgen05 (attend_tc.cu) --------------------------------------------------------

@@ -6,10 +6,11 @@
 // The queries of a unit - rows x heads that share the key head, 16 per row group - meet each stage together, so K and V
 // are read from memory once.  Within a CTA four warps per row group take 16 of a chunk's 64 positions each, with a softmax state of
 // their own, so nothing is exchanged until a unit's part ends.  Parts of units cut over CTAs go to the caller's scratch and are
-// joined by a second, short kernel, in the order of the positions: results do not depend on timing.
+// joined by a second kernel (see attend_parts.cuh).  In small calls
+// every unit has a cluster of CTAs of its own instead, joined through distributed shared memory.
 #include <type_traits>
 
-#include "attend_join.cuh"
+#include "attend_parts.cuh"
 
 namespace stairs {
 namespace att {
@@ -40,6 +41,7 @@ struct Step {
   int first, n, len, qb, h, chunk;      // request's rows and length, block of queries, key head, chunk of positions
   int begins, ends;                     // first step of this CTA's part of the unit; 1: last one, 2: last one and the unit is cut
   int slot;                             // where a cut part goes
+  Cut cut;                              // and who has the others
   unsigned valid[2];                    // positions of the chunk whose page is one
 };
 
@@ -50,7 +52,7 @@ template <int KS, int MG> struct Geo {
   static constexpr int KV = AM_CHUNK * PITCH, STAGE = 2 * KV, QB = ROWS * PITCH, R = NST + 1;
   static constexpr int MERGE_MAX = STAGE / (4 * ROWS * 4) / 8 * 8, MC = MERGE_MAX < HD ? MERGE_MAX : HD;   // columns merged at a time
   static constexpr int SMEM = am_smem(KS, MG, NST);
-  static_assert(sizeof(Step) <= 48 && SMEM <= 227 * 1024, "shared memory");
+  static_assert(sizeof(Step) <= 64 && SMEM <= 227 * 1024, "shared memory");
   static __device__ __forceinline__ uint32_t at(int row, int piece) { return row * PITCH + ((XOR ? piece ^ (row & 7) : piece) << 4); }
 };
 
@@ -64,6 +66,7 @@ __global__ void __launch_bounds__(MG * 128 + 64, am_ctas(KS, MG)) k_attend_mma(c
   Step* steps = reinterpret_cast<Step*>(roff + G::R * AM_CHUNK);                  // [R]
   float* xm = reinterpret_cast<float*>(steps + G::R);                             // [4][ROWS] maxima, then sums
   float* xl = xm + 4 * G::ROWS;
+  float* xm2 = xl + 4 * G::ROWS;                                                  // [2][ROWS] the CTA's own maxima and sums, for its cluster
   __shared__ long long w_sum[G::NT / 32];
   __shared__ int s_req;
   __shared__ long long s_rem;
@@ -73,8 +76,9 @@ __global__ void __launch_bounds__(MG * 128 + 64, am_ctas(KS, MG)) k_attend_mma(c
   wait_prerequisites();
 
   // this CTA's part of the list
-  auto steps_of = [&](const Span& s, int& chunks) -> long long {
-    chunks = max(1, (s.len + AM_CHUNK - 1) / AM_CHUNK);
+  const int S = P.cluster, rank = S ? blockIdx.x % S : 0;
+  auto steps_of = [&](const Span& s, int& chunks) -> long long {   // (where units have CTAs of their own: units)
+    chunks = S ? 1 : max(1, (s.len + AM_CHUNK - 1) / AM_CHUNK);
     return s.n ? ((long long)s.n * group + G::ROWS - 1) / G::ROWS * P.kv_heads * chunks : 0;
   };
   auto scan = [&](long long v, long long& total) {
@@ -92,15 +96,18 @@ __global__ void __launch_bounds__(MG * 128 + 64, am_ctas(KS, MG)) k_attend_mma(c
     total = all;
     return v + before;
   };
-  auto divide = [](long long a, long long b) { return ((a | b) >> 32) == 0 ? (long long)((unsigned)a / (unsigned)b) : a / b; };
   long long total = 0, x0, x1, rem0, parts_all;   // parts_all: CTAs with a part (each has a step at least); rem0: this one's first step, within request req0
   int req0;
   Span span0;
-  Meta* meta = reinterpret_cast<Meta*>(P.ws) + blockIdx.x;
   auto shares = [&]() {
     parts_all = min((long long)gridDim.x, total);
     x0 = x1 = 0;
-    if (blockIdx.x < parts_all) { x0 = divide(total * blockIdx.x, parts_all); x1 = divide(total * (blockIdx.x + 1), parts_all); }
+    if (S) {
+      x0 = blockIdx.x / S;
+      x1 = x0 + (x0 < total);
+      return;
+    }
+    if (blockIdx.x < parts_all) { x0 = share_begin(total, parts_all, blockIdx.x); x1 = share_begin(total, parts_all, blockIdx.x + 1); }
   };
   if (P.n_req <= 32) {                             // every warp by itself
     int chunks;
@@ -115,7 +122,7 @@ __global__ void __launch_bounds__(MG * 128 + 64, am_ctas(KS, MG)) k_attend_mma(c
     }
     total = __shfl_sync(0xffffffffu, incl, 31);
     shares();
-    const unsigned here = __ballot_sync(0xffffffffu, x0 >= incl - v && x0 < incl);
+    const unsigned here = __ballot_sync(0xffffffffu, x1 > x0 && x0 >= incl - v && x0 < incl);
     req0 = here ? __ffs(here) - 1 : 0;
     rem0 = x0 - __shfl_sync(0xffffffffu, incl - v, req0);
     span0.first = __shfl_sync(0xffffffffu, s.first, req0); span0.n = __shfl_sync(0xffffffffu, s.n, req0); span0.len = __shfl_sync(0xffffffffu, s.len, req0);
@@ -140,10 +147,16 @@ __global__ void __launch_bounds__(MG * 128 + 64, am_ctas(KS, MG)) k_attend_mma(c
     if (x1 > x0) { req0 = s_req; rem0 = s_rem; span0 = request_span(P, req0); }
   }
   if (x1 == x0) {
-    if (tid == 0) meta->parts = 0;
+    if (!S && tid == 0) reinterpret_cast<Meta*>(P.ws)[blockIdx.x] = Meta{};
     return;
   }
-  const int n_steps = (int)min(x1 - x0, 0x7fffffffll);
+  int n_steps = (int)min(x1 - x0, 0x7fffffffll), chunk0 = 0;
+  if (S) {                                         // this CTA's range of its unit's chunks
+    const int all = max(1, (span0.len + AM_CHUNK - 1) / AM_CHUNK);
+    chunk0 = (int)((long long)all * rank / S);
+    n_steps = (int)((long long)all * (rank + 1) / S) - chunk0;
+  }
+  auto cluster_sync = []() { __syncwarp(); asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory"); };
 
   const uint32_t sm0 = smem_addr(am_sm), q0 = smem_addr(qring);
   if (warp >= MG * 4) {
@@ -153,9 +166,8 @@ __global__ void __launch_bounds__(MG * 128 + 64, am_ctas(KS, MG)) k_attend_mma(c
     Span sp = span0;
     auto units_of = [&](const Span& s) { chunks = max(1, (s.len + AM_CHUNK - 1) / AM_CHUNK); return (int)(((long long)s.n * group + G::ROWS - 1) / G::ROWS) * P.kv_heads; };
     int units = units_of(sp);
-    unit = (int)divide(rem0, chunks); chunk = (int)(rem0 - (long long)unit * chunks);
-    Meta end_meta{};
-    long long end_at = 0;                       // where the unit that goes on in the next CTAs ends
+    if (S) { unit = (int)rem0; chunk = chunk0; }
+    else { unit = (int)divide(rem0, chunks); chunk = (int)(rem0 - (long long)unit * chunks); }
     int seg = 0, part_begin = chunk, planned = 0;
     Step plan;                                  // the step being planned, and this thread's position's place
     long long place = -1;
@@ -165,7 +177,7 @@ __global__ void __launch_bounds__(MG * 128 + 64, am_ctas(KS, MG)) k_attend_mma(c
       plan.qb = unit / P.kv_heads; plan.h = unit - plan.qb * P.kv_heads; plan.chunk = chunk;
       plan.begins = chunk == part_begin;
       const bool unit_ends = chunk + 1 == chunks, last = planned + 1 == n_steps;
-      plan.ends = (unit_ends || last) ? ((part_begin > 0 || !unit_ends) ? 2 : 1) : 0;
+      plan.ends = (unit_ends || last) && !S ? ((part_begin > 0 || !unit_ends) ? 2 : 1) : 0;
       plan.slot = 2 * blockIdx.x + (seg ? 1 : 0);
       const int p = chunk * AM_CHUNK + ct;
       place = -1;
@@ -173,10 +185,7 @@ __global__ void __launch_bounds__(MG * 128 + 64, am_ctas(KS, MG)) k_attend_mma(c
         const int b = p / P.page_tokens, page = __ldg(P.table + (size_t)req * P.max_blocks + b);
         if (page >= 0 && page < P.n_pages) place = page * P.page_stride + (p - b * P.page_tokens) * P.token_stride;
       }
-      if (last && plan.ends == 2 && part_begin == 0) {
-        end_meta.slot = plan.slot; end_meta.first = sp.first; end_meta.n = sp.n; end_meta.qb = plan.qb; end_meta.h = plan.h;
-        end_at = x1 + (chunks - 1 - chunk);
-      }
+      if (plan.ends == 2) { const long long u0 = x0 + planned - chunk; plan.cut = cut_of(u0, u0 + chunks, total, parts_all); }
       if (unit_ends) {
         chunk = 0; ++seg; part_begin = 0;
         if (++unit == units && !last) {
@@ -195,7 +204,7 @@ __global__ void __launch_bounds__(MG * 128 + 64, am_ctas(KS, MG)) k_attend_mma(c
         if (lane == 0) s->valid[ct >> 5] = v;
         if (ct == 0) {
           s->first = plan.first; s->n = plan.n; s->len = plan.len; s->qb = plan.qb; s->h = plan.h; s->chunk = plan.chunk;
-          s->begins = plan.begins; s->ends = plan.ends; s->slot = plan.slot;
+          s->begins = plan.begins; s->ends = plan.ends; s->slot = plan.slot; s->cut = plan.cut;
         }
         ++planned;
       }
@@ -254,29 +263,83 @@ __global__ void __launch_bounds__(MG * 128 + 64, am_ctas(KS, MG)) k_attend_mma(c
       plan_store();
     }
     cp_wait<0>();
-    if (ct == 0) {
-      if (end_at) {
-        // the CTA that holds the unit's last step: the first whose part ends behind it
-        long long e = divide(end_at * parts_all - 1, total);           // (about; corrected below)
-        while (e > 0 && divide(total * e, parts_all) >= end_at) --e;
-        while (divide(total * (e + 1), parts_all) < end_at) ++e;
-        end_meta.parts = (int)(e - blockIdx.x) + 1;
-      }
-      *meta = end_meta;
-    }
-    return;
-  }
-
+    if (S > 1) { cluster_sync(); cluster_sync(); }
+  } else {
   // ------------------------------------------------------------------ computing warps
   const float sc = P.scale * 1.4426950408889634f;                  // exponentials in base 2
   auto group_sync = []() { asm volatile("bar.sync 1, %0;" ::"n"(MG * 128) : "memory"); };
-  float acc[KS * 2][4], m_run[2], l_run[2];
+  float acc[KS * 2][4], m_run[2] = {-INFINITY, -INFINITY}, l_run[2] = {0.f, 0.f};
   int cur_unit = -1, last0 = 0, last1 = 0;
+  Meta unit{};                                                     // (thread 0)
+  const int row0 = mg * 16 + (lane >> 2);                          // this thread's rows: row0 and row0 + 8
+  auto put = [&](int row, int head, int c, const float4& o, float inv) {
+    uint2 u;
+    u.x = pack2<T>(o.x * inv, o.y * inv); u.y = pack2<T>(o.z * inv, o.w * inv);
+    *reinterpret_cast<uint2*>(reinterpret_cast<T*>(P.o) + row * P.o_row + head * P.o_head + c) = u;
+  };
+  // The four warps of a row group: common maximum, then sums, through a stage that is free; to(row, column, four values, maximum, sum).
+  auto merge = [&](int stage, auto&& to) {
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+      l_run[e] += __shfl_xor_sync(0xffffffffu, l_run[e], 1);
+      l_run[e] += __shfl_xor_sync(0xffffffffu, l_run[e], 2);
+    }
+    if ((lane & 3) == 0) {
+      xm[pw * G::ROWS + row0] = m_run[0]; xm[pw * G::ROWS + row0 + 8] = m_run[1];
+      xl[pw * G::ROWS + row0] = l_run[0]; xl[pw * G::ROWS + row0 + 8] = l_run[1];
+    }
+    group_sync();
+    float f[2];
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+      float M = -INFINITY;
+#pragma unroll
+      for (int w = 0; w < 4; ++w) M = fmaxf(M, xm[w * G::ROWS + row0 + 8 * e]);
+      f[e] = m_run[e] == -INFINITY ? 0.f : ex2(m_run[e] - M);
+    }
+    float* mt = reinterpret_cast<float*>(am_sm + stage * G::STAGE);                // [4][ROWS][MC]
+    for (int col0 = 0; col0 < P.hd; col0 += G::MC) {
+#pragma unroll
+      for (int d = 0; d < KS * 2; ++d) {
+        const int col = d * 8 + (lane & 3) * 2 - col0;
+        if (col >= 0 && col < G::MC) {
+          float* at0 = mt + ((size_t)pw * G::ROWS + row0) * G::MC + col;
+          *reinterpret_cast<float2*>(at0) = make_float2(f[0] != 0.f ? acc[d][0] * f[0] : 0.f, f[0] != 0.f ? acc[d][1] * f[0] : 0.f);
+          *reinterpret_cast<float2*>(at0 + 8 * G::MC) = make_float2(f[1] != 0.f ? acc[d][2] * f[1] : 0.f, f[1] != 0.f ? acc[d][3] * f[1] : 0.f);
+        }
+      }
+      group_sync();
+      const int cols = min(G::MC, P.hd - col0);                    // (both are multiples of 8)
+      for (int it = tid; it < G::ROWS * (G::MC / 4); it += G::NC) {
+        const int r = it / (G::MC / 4), c = it % (G::MC / 4) * 4;
+        if (c >= cols) continue;
+        float M = -INFINITY, L = 0.f;
+#pragma unroll
+        for (int w = 0; w < 4; ++w) M = fmaxf(M, xm[w * G::ROWS + r]);
+#pragma unroll
+        for (int w = 0; w < 4; ++w) { const float mw = xm[w * G::ROWS + r]; L += mw == -INFINITY ? 0.f : xl[w * G::ROWS + r] * ex2(mw - M); }
+        float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+          const float4 v = *reinterpret_cast<const float4*>(mt + ((size_t)w * G::ROWS + r) * G::MC + c);
+          o.x += v.x; o.y += v.y; o.z += v.z; o.w += v.w;
+        }
+        to(r, col0 + c, o, M, L);
+      }
+      group_sync();
+    }
+  };
+  if (n_steps == 0) {                                              // (shared units only)
+#pragma unroll
+    for (int i = 0; i < KS * 2; ++i)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) acc[i][j] = 0.f;
+  }
   for (int x = 0; x < n_steps; ++x) {
     __syncthreads();
     const Step& s = steps[x % G::R];
     const int s_first = s.first, s_n = s.n, s_len = s.len, s_qb = s.qb, s_h = s.h, s_ends = s.ends, s_slot = s.slot;
-    const int r0 = mg * 16 + (lane >> 2), qi0 = s_qb * G::ROWS + r0, qi1 = qi0 + 8;
+    const int qi0 = s_qb * G::ROWS + row0, qi1 = qi0 + 8;
     if (s.begins) {
       ++cur_unit;
 #pragma unroll
@@ -390,67 +453,70 @@ __global__ void __launch_bounds__(MG * 128 + 64, am_ctas(KS, MG)) k_attend_mma(c
       }
     }
     if (s_ends) {
-      // the four warps of a row group: common maximum, then sums, through the stage just consumed
-#pragma unroll
-      for (int e = 0; e < 2; ++e) {
-        l_run[e] += __shfl_xor_sync(0xffffffffu, l_run[e], 1);
-        l_run[e] += __shfl_xor_sync(0xffffffffu, l_run[e], 2);
-      }
-      if ((lane & 3) == 0) {
-        xm[pw * G::ROWS + r0] = m_run[0]; xm[pw * G::ROWS + r0 + 8] = m_run[1];
-        xl[pw * G::ROWS + r0] = l_run[0]; xl[pw * G::ROWS + r0 + 8] = l_run[1];
-      }
-      group_sync();
-      float f[2];
-#pragma unroll
-      for (int e = 0; e < 2; ++e) {
-        float M = -INFINITY;
-#pragma unroll
-        for (int w = 0; w < 4; ++w) M = fmaxf(M, xm[w * G::ROWS + r0 + 8 * e]);
-        f[e] = m_run[e] == -INFINITY ? 0.f : ex2(m_run[e] - M);
-      }
-      float* mt = reinterpret_cast<float*>(am_sm + (x % NST) * G::STAGE);          // [4][ROWS][MC]
-      float* part = reinterpret_cast<float*>(reinterpret_cast<unsigned char*>(P.ws) + (size_t)gridDim.x * sizeof(Meta)) + s_slot * (size_t)(G::ROWS * (P.hd + 2));
-      for (int col0 = 0; col0 < P.hd; col0 += G::MC) {
-#pragma unroll
-        for (int d = 0; d < KS * 2; ++d) {
-          const int col = d * 8 + (lane & 3) * 2 - col0;
-          if (col >= 0 && col < G::MC) {
-            float* at0 = mt + ((size_t)pw * G::ROWS + r0) * G::MC + col;
-            *reinterpret_cast<float2*>(at0) = make_float2(f[0] != 0.f ? acc[d][0] * f[0] : 0.f, f[0] != 0.f ? acc[d][1] * f[0] : 0.f);
-            *reinterpret_cast<float2*>(at0 + 8 * G::MC) = make_float2(f[1] != 0.f ? acc[d][2] * f[1] : 0.f, f[1] != 0.f ? acc[d][3] * f[1] : 0.f);
-          }
-        }
-        group_sync();
-        const int cols = min(G::MC, P.hd - col0);                  // (both are multiples of 8)
-        for (int it = tid; it < G::ROWS * (G::MC / 4); it += G::NC) {
-          const int r = it / (G::MC / 4), c = it % (G::MC / 4) * 4, qi = s_qb * G::ROWS + r, j = qi / group;
-          if (c >= cols || j >= s_n) continue;
-          float M = -INFINITY, L = 0.f;
-#pragma unroll
-          for (int w = 0; w < 4; ++w) M = fmaxf(M, xm[w * G::ROWS + r]);
-#pragma unroll
-          for (int w = 0; w < 4; ++w) { const float mw = xm[w * G::ROWS + r]; L += mw == -INFINITY ? 0.f : xl[w * G::ROWS + r] * ex2(mw - M); }
-          float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll
-          for (int w = 0; w < 4; ++w) {
-            const float4 v = *reinterpret_cast<const float4*>(mt + ((size_t)w * G::ROWS + r) * G::MC + c);
-            o.x += v.x; o.y += v.y; o.z += v.z; o.w += v.w;
-          }
-          if (s_ends == 2) {
-            *reinterpret_cast<float4*>(part + (size_t)r * P.hd + col0 + c) = o;
-            if (c == 0 && col0 == 0) { part[(size_t)G::ROWS * P.hd + r] = M; part[(size_t)G::ROWS * (P.hd + 1) + r] = L; }
-          } else {
-            const float inv = M == -INFINITY ? 0.f : 1.f / L;
-            T* dst = reinterpret_cast<T*>(P.o) + (s_first + j) * P.o_row + (s_h * group + qi - j * group) * P.o_head + col0 + c;
-            uint2 u;
-            u.x = pack2<T>(o.x * inv, o.y * inv); u.y = pack2<T>(o.z * inv, o.w * inv);
-            *reinterpret_cast<uint2*>(dst) = u;
-          }
-        }
-        group_sync();
-      }
+      const size_t slot_floats = (size_t)G::ROWS * (P.hd + 2);
+      float* part = const_cast<float*>(parts_of(P, gridDim.x)) + s_slot * slot_floats;
+      merge(x % NST, [&](int r, int c, const float4& o, float M, float L) {
+        const int qi = s_qb * G::ROWS + r, j = qi / group;
+        if (j >= s_n) return;
+        if (s_ends == 2) {
+          *reinterpret_cast<float4*>(part + (size_t)r * P.hd + c) = o;
+          if (c == 0) { part[(size_t)G::ROWS * P.hd + r] = M; part[(size_t)G::ROWS * (P.hd + 1) + r] = L; }
+        } else put(s_first + j, s_h * group + qi - j * group, c, o, M == -INFINITY ? 0.f : 1.f / L);
+      });
+      if (s_ends == 2 && tid == 0 && steps[x % G::R].cut.owner == (int)blockIdx.x) unit = Meta{steps[x % G::R].cut, s_first, s_n, s_qb, s_h, 0};
     }
+  }
+  if (!S && tid == 0) reinterpret_cast<Meta*>(P.ws)[blockIdx.x] = unit;
+
+  if (S) {
+    const int qb = (int)rem0 / P.kv_heads, h = (int)rem0 - qb * P.kv_heads, rows = min(G::ROWS, span0.n * group - qb * G::ROWS);
+    if (S == 1) {
+      merge(0, [&](int r, int c, const float4& o, float M, float L) {
+        const int qi = qb * G::ROWS + r, j = qi / group;
+        if (r < rows) put(span0.first + j, h * group + qi - j * group, c, o, M == -INFINITY ? 0.f : 1.f / L);
+      });
+    } else {
+    // this CTA's state, whole, where the others find it: values in the second stage (none of them is in use any more), maxima and sums behind them
+    float* xo = reinterpret_cast<float*>(am_sm + G::STAGE);
+    merge(0, [&](int r, int c, const float4& o, float M, float L) {
+      *reinterpret_cast<float4*>(xo + (size_t)r * P.hd + c) = o;
+      if (c == 0) { xm2[r] = M; xm2[G::ROWS + r] = L; }
+    });
+    cluster_sync();
+    const int q4 = P.hd / 4;
+    for (int it = rank * G::NC + tid; it < rows * q4; it += S * G::NC) {
+      const int r = it / q4, c = it % q4 * 4, qi = qb * G::ROWS + r, j = qi / group;
+      const uint32_t am = smem_addr(xm2 + r), ao = smem_addr(xo + (size_t)r * P.hd + c);
+      float m[8], M = -INFINITY, L = 0.f;
+#pragma unroll
+      for (int p = 0; p < 8; ++p) {
+        m[p] = -INFINITY;
+        if (p < S) {
+          uint32_t at;
+          asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"(am), "r"(p));
+          asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(m[p]) : "r"(at));
+        }
+        M = fmaxf(M, m[p]);
+      }
+      float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+      for (int p = 0; p < 8; ++p) {
+        if (m[p] == -INFINITY) continue;
+        uint32_t at_l, at_o;
+        float l;
+        float4 v;
+        asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at_l) : "r"(am + G::ROWS * 4), "r"(p));
+        asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at_o) : "r"(ao), "r"(p));
+        asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(l) : "r"(at_l));
+        asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(at_o));
+        const float w = ex2(m[p] - M);
+        if (w != 0.f) { L = fmaf(l, w, L); o.x = fmaf(v.x, w, o.x); o.y = fmaf(v.y, w, o.y); o.z = fmaf(v.z, w, o.z); o.w = fmaf(v.w, w, o.w); }
+      }
+      put(span0.first + j, h * group + qi - j * group, c, o, M == -INFINITY ? 0.f : 1.f / L);
+    }
+    cluster_sync();                                                // (a CTA's shared memory is there until all have read it)
+    }
+  }
   }
 }
 
@@ -459,9 +525,20 @@ template <typename T, int KS, int MG> int launch(const AttendParams& P, cudaStre
   auto kern = k_attend_mma<T, KS, MG>;
   static std::atomic<unsigned long long> done{0};
   if (int rc = allow_shared(done, reinterpret_cast<const void*>(kern), G::SMEM)) return rc;
-  kern<<<am_grid(KS, MG), G::NT, G::SMEM, st>>>(P);
-  SCK(cudaGetLastError());
-  return launch_join<T, MG * 16>(P, am_grid(KS, MG), 4, st);
+  if (P.cluster == 0) {
+    kern<<<am_grid(KS, MG), G::NT, G::SMEM, st>>>(P);
+    SCK(cudaGetLastError());
+    return launch_join<T, G::ROWS, false>(P, am_grid(KS, MG), st);
+  }
+  const long long q = (long long)P.n_rows * (P.heads / P.kv_heads), blocks = P.n_req == 1 ? (q + G::ROWS - 1) / G::ROWS : q / G::ROWS + P.n_req;
+  cudaLaunchConfig_t cfg{};
+  cfg.gridDim = dim3((unsigned)(blocks * P.kv_heads * P.cluster)); cfg.blockDim = dim3(G::NT); cfg.dynamicSmemBytes = G::SMEM; cfg.stream = st;
+  cudaLaunchAttribute at[1];
+  at[0].id = cudaLaunchAttributeClusterDimension;
+  at[0].val.clusterDim.x = P.cluster; at[0].val.clusterDim.y = 1; at[0].val.clusterDim.z = 1;
+  cfg.attrs = at; cfg.numAttrs = P.cluster > 1 ? 1 : 0;
+  SCK(cudaLaunchKernelEx(&cfg, kern, P));
+  return STAIRS_OK;
 }
 
 template <typename T> int launch_mg(const AttendParams& P, int mg, cudaStream_t st) {

@@ -1,0 +1,122 @@
+// Units of attention that are cut over CTAs: who has which part, and who joins them.
+//
+// The steps of a call lie in one list, cut into shares of equal length, so a unit's parts lie in consecutive CTAs.  A CTA files its part's
+// state (maxima, sums, weighted values) in its scratch; a second, short kernel joins the parts, in the order of the positions, so results do not depend
+// on timing.  (Measured against joins by the CTA that is the last to file a part: four requests of 16384, one token each, 64 us against 79; one request, heads of 64, 32
+// against 43.  Where units are of 256 queries and have two or three parts, the last one joins from its registers: a chunk of 2048 rows 233 us with the kernel, 224 without.)
+#pragma once
+#include <type_traits>
+
+#include "attend.cuh"
+
+namespace stairs {
+namespace att {
+namespace {
+
+template <typename T> __device__ __forceinline__ uint32_t pack2(float lo, float hi) {
+  uint32_t r;
+  if (std::is_same<T, bf16>::value) asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+  else asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+  return r;
+}
+__device__ __forceinline__ float ex2(float x) { return exp2f(x); }
+
+__device__ __forceinline__ long long divide(long long a, long long b) { return ((a | b) >> 32) == 0 ? (long long)((unsigned)a / (unsigned)b) : a / b; }
+// first step of CTA b's share of `total` steps over `ctas` CTAs
+__device__ __forceinline__ long long share_begin(long long total, long long ctas, long long b) { return divide(total * b, ctas); }
+// the CTA whose share holds step x
+__device__ __forceinline__ int share_of(long long total, long long ctas, long long x) {
+  long long b = divide(x * ctas, total);          // (about; corrected below)
+  while (b > 0 && share_begin(total, ctas, b) > x) --b;
+  while (b + 1 < ctas && share_begin(total, ctas, b + 1) <= x) ++b;
+  return (int)b;
+}
+
+// A cut unit of steps [u0, u1): its parts lie in CTAs owner .. owner + parts - 1.  Every CTA has two places for states: one for the part that its share
+// begins with, one for a part that it begins later (and ends with).
+struct Cut {
+  int owner, parts, slot0;
+  __device__ __forceinline__ int slot(int p) const { return p ? 2 * (owner + p) : slot0; }
+};
+__device__ __forceinline__ Cut cut_of(long long u0, long long u1, long long total, long long ctas) {
+  Cut c;
+  c.owner = share_of(total, ctas, u0);
+  c.parts = share_of(total, ctas, u1 - 1) - c.owner + 1;
+  c.slot0 = 2 * c.owner + (u0 != share_begin(total, ctas, c.owner) ? 1 : 0);
+  return c;
+}
+
+// The unit that a CTA begins and does not end (parts 0: none), and whether the CTA gave up a wait.
+struct Meta { Cut cut; int first, n, qb, h, failed; };
+__device__ __forceinline__ const float* parts_of(const AttendParams& P, int ctas) {
+  return reinterpret_cast<const float*>(reinterpret_cast<const unsigned char*>(P.ws) + ((size_t)ctas * sizeof(Meta) + 255) / 256 * 256);
+}
+
+// State of a part: values of ROWS rows (COLS: [column / 4][row][4], else [row][head]), maxima, sums.  Block x: the unit of CTA x; y: a share of it.
+template <typename T, int ROWS, bool COLS> __global__ void __launch_bounds__(128) k_attend_join(const __grid_constant__ AttendParams P) {
+  wait_prerequisites();
+  const Meta* metas = reinterpret_cast<const Meta*>(P.ws);
+  const Meta u = metas[blockIdx.x];
+  if (COLS) {
+    // a part whose CTA gave up a wait (which takes a broken device) is no part: nothing of the call counts, and every row says so
+    int bad = 0;
+    for (int i = threadIdx.x; i < gridDim.x; i += 128) bad |= metas[i].failed;
+    if (__syncthreads_or(bad)) {
+      const long long all = (long long)P.n_rows * P.heads;
+      for (long long r = (long long)blockIdx.y * gridDim.x + blockIdx.x; r < all; r += (long long)gridDim.x * gridDim.y)
+        for (int d = threadIdx.x; d < P.hd; d += 128) reinterpret_cast<T*>(P.o)[(r / P.heads) * P.o_row + (r % P.heads) * P.o_head + d] = from_f32<T>(NAN);
+      return;
+    }
+  }
+  if (u.cut.parts == 0) return;
+  const int group = P.heads / P.kv_heads, q4 = P.hd / 4, rows = min(ROWS, u.n * group - u.qb * ROWS);
+  const size_t slot_floats = (size_t)ROWS * (P.hd + 2);
+  const float* parts = parts_of(P, gridDim.x);
+  for (int it = blockIdx.y * 128 + threadIdx.x; it < rows * q4; it += gridDim.y * 128) {
+    const int r = COLS ? it % rows : it / q4, c = (COLS ? it / rows : it % q4) * 4, qi = u.qb * ROWS + r, j = qi / group;
+    float M = -INFINITY, L = 0.f;
+    float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+    // eight parts' loads under way together
+    for (int p0 = 0; p0 < u.cut.parts; p0 += 8) {
+      float mp[8], lp[8];
+      float4 v[8];
+#pragma unroll
+      for (int k = 0; k < 8; ++k) {
+        const bool on = p0 + k < u.cut.parts;
+        const float* s0 = parts + u.cut.slot(on ? p0 + k : 0) * slot_floats;
+        mp[k] = on ? s0[(size_t)ROWS * P.hd + r] : -INFINITY;
+        lp[k] = s0[(size_t)ROWS * (P.hd + 1) + r];
+        v[k] = *reinterpret_cast<const float4*>(s0 + (COLS ? ((size_t)c / 4 * ROWS + r) * 4 : (size_t)r * P.hd + c));
+      }
+      float m = M;
+#pragma unroll
+      for (int k = 0; k < 8; ++k) m = fmaxf(m, mp[k]);
+      const float f = M == -INFINITY ? 0.f : ex2(M - m);
+      M = m;
+      L *= f; o.x *= f; o.y *= f; o.z *= f; o.w *= f;
+#pragma unroll
+      for (int k = 0; k < 8; ++k) {
+        const float w = mp[k] == -INFINITY ? 0.f : ex2(mp[k] - m);
+        if (w != 0.f) { L = fmaf(lp[k], w, L); o.x = fmaf(v[k].x, w, o.x); o.y = fmaf(v[k].y, w, o.y); o.z = fmaf(v[k].z, w, o.z); o.w = fmaf(v[k].w, w, o.w); }
+      }
+    }
+    const float inv = M == -INFINITY ? 0.f : 1.f / L;
+    uint2 y;
+    y.x = pack2<T>(o.x * inv, o.y * inv); y.y = pack2<T>(o.z * inv, o.w * inv);
+    *reinterpret_cast<uint2*>(reinterpret_cast<T*>(P.o) + (u.first + j) * P.o_row + (u.h * group + qi - j * group) * P.o_head + c) = y;
+  }
+}
+
+template <typename T, int ROWS, bool COLS> int launch_join(const AttendParams& P, int ctas, cudaStream_t st) {
+  cudaLaunchConfig_t cfg{};
+  cfg.gridDim = dim3(ctas, 4); cfg.blockDim = dim3(128); cfg.stream = st;
+  cudaLaunchAttribute at[1];
+  at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization; at[0].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = at; cfg.numAttrs = 1;
+  SCK(cudaLaunchKernelEx(&cfg, k_attend_join<T, ROWS, COLS>, P));
+  return STAIRS_OK;
+}
+
+}  // namespace
+}  // namespace att
+}  // namespace stairs

@@ -4,18 +4,22 @@
 // and 1024 of its special-function units.  So a CTA works on two tiles of 128 queries at a time: while one tile's softmax runs, the other's products do.
 //   S = Q.K^T (M = N = 128) -> TMEM; one thread per query takes its row into registers, writes the weights back over it as 16-bit
 //   values, and O += P.V takes them from there as the A operand, V as copied (positions are the MMA's K, so V is MN-major).
+// A unit of at most 128 queries is bound by reading K and V: both tiles then take its queries, one the even chunks and one the odd ones, and
+// their states are merged at the unit's end.
+// The issuing thread is nearly as busy as the tensor pipe (about 50 cycles an instruction, 240 a commit): it commits only what the softmax
+// waits for, and the softmax threads, which so know what has completed, hand the K and V stages back.
 // TMEM: S of two tiles (128 columns each) and O of two tiles: all 512 columns, one CTA per SM.
 // Warps: 0-3 and 4-7 softmax of a tile each, 8 K/V copies (tiled TMA, one box per page slice and 64 columns; pages that are none lie
 // outside the tensor and arrive as zeros), 9 MMA issue and TMEM, 10-11 queries (16-byte asynchronous copies: any strides) and the values of chunks that
 // reach past some query's last position: what lies behind the request's end is cleared, and infinities and NaN are taken out, since
 // 0 * infinity in a product would carry them to rows that do not see them; rows that do get them added at the end.
 // The steps (request, 256 queries, key head, 128 positions; only visible ones) form one list, cut evenly over the CTAs; units cut over
-// CTAs are joined by a second kernel.
+// CTAs are joined by a second kernel, or, wide, 32 queries at a time by the warp that is the last to have its part (see attend_parts.cuh).
 #include <cuda.h>
 
 #include <type_traits>
 
-#include "attend_join.cuh"
+#include "attend_parts.cuh"
 #include "gemm_tc.cuh"
 
 namespace stairs {
@@ -24,7 +28,7 @@ namespace {
 
 using namespace tc;
 
-constexpr int AT_CH = 128, AT_THREADS = 384, AT_ROWS = 256, AT_STAGES = 2, AT_RING = 4;
+constexpr int AT_THREADS = 384, AT_RING = 8, AT_PARTS = 4;   // (rings of numbers that travel beside the stages: of chunks, of parts)
 constexpr unsigned long long AT_WAIT = 4000000000ull;   // cycles (two seconds) after which a wait gives up
 
 struct TcParams {
@@ -95,27 +99,44 @@ __device__ __forceinline__ float ex2a(float x) {
 // A unit: 256 queries of a request that share a key head.  Tile t has queries qb * 256 + 128 t ..; it sees its first `n_t` chunks.
 struct Unit { int req, first, n, len, qb, h, nch[2], all, c; };   // all: chunks of the unit (1 where nothing is seen), c: the next one
 
-__device__ __forceinline__ int tile_chunks(int n, int len, int q0, int group) {
-  const int nq = min(n * group - q0, 128);
-  if (nq <= 0) return 0;
-  const int last = len - n + (q0 + nq - 1) / group;
-  return last < 0 ? 0 : last / AT_CH + 1;
-}
-__device__ __forceinline__ void unit_sizes(Unit& u, int group) {
-  u.nch[0] = tile_chunks(u.n, u.len, u.qb * AT_ROWS, group);
-  u.nch[1] = tile_chunks(u.n, u.len, u.qb * AT_ROWS + 128, group);
-  u.all = max(1, max(u.nch[0], u.nch[1]));
-}
+// The two forms.  Wide: 256 queries a unit, a tile each 128, chunks of 128 positions (the fewest instructions for the work), two stages.  Narrow: 128
+// queries, both tiles on them, chunks of 64 positions in more stages: K and V are what it waits for.
+template <bool NARROW> struct Form {
+  static constexpr int CH = NARROW ? 64 : 128, ROWS = NARROW ? 128 : 256, NST = NARROW ? 5 : 2, Q_TILES = NARROW ? 1 : 2;
+  static __device__ __forceinline__ int tile_chunks(int n, int len, int q0, int group) {
+    const int nq = min(n * group - q0, 128);
+    if (nq <= 0) return 0;
+    const int last = len - n + (q0 + nq - 1) / group;
+    return last < 0 ? 0 : last / CH + 1;
+  }
+  static __device__ __forceinline__ void sizes(Unit& u, int group) {
+    u.nch[0] = tile_chunks(u.n, u.len, u.qb * ROWS, group);
+    u.nch[1] = NARROW ? 0 : tile_chunks(u.n, u.len, u.qb * ROWS + 128, group);
+    u.all = max(1, max(u.nch[0], u.nch[1]));
+  }
+  static __device__ __forceinline__ int blocks_of(int n, int group) { return (int)(((long long)n * group + ROWS - 1) / ROWS); }
+};
 __device__ __forceinline__ void unit_load(Unit& u, const AttendParams& P, int req) {
   const Span s = request_span(P, req);
   u.req = req; u.first = s.first; u.n = s.n; u.len = s.len;
 }
-__device__ __forceinline__ int blocks_of(int n, int group) { return (int)(((long long)n * group + AT_ROWS - 1) / AT_ROWS); }
+template <int HD, bool NARROW> constexpr int at_smem() {
+  typedef Form<NARROW> F;
+  return 1024 + F::Q_TILES * 128 * HD * 2 + F::NST * 2 * F::CH * HD * 2 + 512 + (NARROW ? 4 : 8) * 32 * 20 * 4 + (NARROW ? 128 * 36 * 4 + 1024 : 0);
+}
 
-template <int HD> constexpr int at_smem() { return 1024 + AT_ROWS * HD * 2 + AT_STAGES * 2 * AT_CH * HD * 2 + 512; }
+// How the two tiles share a part of L chunks from c0 on.
+template <bool NARROW> struct Share {
+  int L, n[2];                                     // n[t]: chunks of tile t; narrow: chunk j is tile j % 2's, else every tile's that sees it
+  __device__ __forceinline__ Share(const Unit& u, int c0, int c1) {
+    n[0] = max(0, min(c1, u.nch[0]) - c0); n[1] = max(0, min(c1, u.nch[1]) - c0);
+    L = max(n[0], n[1]);
+    if (NARROW) { n[0] = (L + 1) / 2; n[1] = L / 2; }
+  }
+};
 
 // A CTA's walk over its part of the list; every role keeps one.
-struct Walk {
+template <bool NARROW> struct Walk {
   Unit u;
   long long left;
   int seg;
@@ -133,24 +154,27 @@ struct Walk {
     u.c = 0;                                        // (a part that ends inside a unit is the CTA's last one)
     if (++u.h == P.kv_heads) {
       u.h = 0;
-      if (++u.qb == blocks_of(u.n, group)) {
+      if (++u.qb == Form<NARROW>::blocks_of(u.n, group)) {
         u.qb = 0;
         int r = u.req;
         do { unit_load(u, P, ++r); } while (u.n == 0);   // (there are steps left, so there is such a request)
       }
-      unit_sizes(u, group);
+      Form<NARROW>::sizes(u, group);
     }
   }
 };
 
-template <typename T, int HD>
+template <typename T, int HD, bool NARROW>
 __global__ void __launch_bounds__(AT_THREADS, 1) k_attend_tc(const __grid_constant__ TcParams J) {
   constexpr bool BF = std::is_same<T, bf16>::value;
-  constexpr int HALVES = HD / 64, KBYTES = AT_CH * HD * 2, QTILE = 128 * HD * 2, NST = AT_STAGES;
+  typedef Form<NARROW> F;
+  typedef Share<NARROW> Sh;
+  constexpr int AT_CH = F::CH, AT_ROWS = F::ROWS, NST = F::NST;
+  constexpr int HALVES = HD / 64, KBYTES = AT_CH * HD * 2, QTILE = 128 * HD * 2;
   extern __shared__ __align__(1024) uint8_t at_raw[];
   const AttendParams& P = J.a;
-  uint8_t* qs = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(at_raw) + 1023) & ~(uintptr_t)1023);   // 2 tiles x HALVES x [128][128 bytes]
-  uint8_t* kst = qs + 2 * QTILE;                    // stages of K, then of V: HALVES x [128][128 bytes]
+  uint8_t* qs = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(at_raw) + 1023) & ~(uintptr_t)1023);   // tiles x HALVES x [128][128 bytes]
+  uint8_t* kst = qs + F::Q_TILES * QTILE;           // stages of K, then of V: HALVES x [positions][128 bytes]
   uint8_t* vst = kst + NST * KBYTES;
   uint64_t* k_full = reinterpret_cast<uint64_t*>(vst + NST * KBYTES);
   uint64_t* k_empty = k_full + NST; uint64_t* v_full = k_empty + NST; uint64_t* v_empty = v_full + NST;
@@ -158,89 +182,144 @@ __global__ void __launch_bounds__(AT_THREADS, 1) k_attend_tc(const __grid_consta
   uint64_t* q_full = v_fixed + NST; uint64_t* q_empty = q_full + 1;
   uint64_t* s_full = q_empty + 1;                   // [2 tiles]
   uint64_t* p_full = s_full + 2; uint64_t* o_full = p_full + 2; uint64_t* o_free = o_full + 2;
-  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(o_free + 2);
+  uint64_t* x_full = o_free + 2;                    // columns of the second tile's state are written, and have been read
+  uint64_t* x_free = x_full + 1;
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(x_free + 1);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
-  volatile unsigned* valid_ring = reinterpret_cast<volatile unsigned*>(tmem_slot + 4);   // [4] page slices of a chunk that exist
+  volatile unsigned* valid_ring = reinterpret_cast<volatile unsigned*>(tmem_slot + 4);   // [8] page slices of a chunk that exist
   volatile int* odd_ring = reinterpret_cast<volatile int*>(valid_ring + AT_RING);        // [4][2 warps] parts whose values had infinities or NaN taken out
+  float* xch = reinterpret_cast<float*>(reinterpret_cast<uint8_t*>(k_full) + 512);      // [warps that store][32][20]
+  float* other = xch + (NARROW ? 4 : 8) * (32 * 20);                                    // narrow: the second tile's state on its way to the first: [128 queries][36], 32 columns at a time
+  float* other_ml = other + 128 * 36;                                                   // its maxima and sums
   __shared__ long long w_sum[AT_THREADS / 32];
-  __shared__ Walk s_walk;
+  __shared__ Meta s_meta;
+  __shared__ Walk<NARROW> s_walk, walks[AT_THREADS / 32];   // every warp's own walk (in shared memory: the softmax has no registers to spare)
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int group = P.heads / P.kv_heads;
   launch_dependents();
   wait_prerequisites();
   if (tid == 0) {
     for (int s = 0; s < NST; ++s) { mbar_init(k_full + s, 1); mbar_init(k_empty + s, 1); mbar_init(v_full + s, 1); mbar_init(v_empty + s, 1); mbar_init(v_fixed + s, 2); }
-    mbar_init(q_full, 2); mbar_init(q_empty, 1);
+    mbar_init(q_full, 2); mbar_init(q_empty, 1); mbar_init(x_full, 4); mbar_init(x_free, 4);
     for (int t = 0; t < 2; ++t) { mbar_init(s_full + t, 1); mbar_init(p_full + t, 4); mbar_init(o_full + t, 1); mbar_init(o_free + t, 4); }
     *abort_flag = 0;
-    for (int i = 0; i < 2 * AT_RING; ++i) odd_ring[i] = 0;
+    s_meta = Meta{};
+    for (int i = 0; i < 2 * AT_PARTS; ++i) odd_ring[i] = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
   // this CTA's part of the list
-  auto steps_of = [&](int i) -> long long {
-    Unit u;
-    unit_load(u, P, i);
-    long long n = 0;
-    const int blocks = blocks_of(u.n, group);
-    for (u.qb = 0; u.qb < blocks; ++u.qb) { unit_sizes(u, group); n += u.all; }
-    return n * P.kv_heads;
+  auto unit_steps = [&](const Span& sp, int qb) {            // chunks of the units of block qb, one for each key head
+    const int last = sp.len - sp.n + (int)((unsigned)(min(sp.n * group, (qb + 1) * AT_ROWS) - 1) / (unsigned)group);
+    return last < 0 ? 1 : last / AT_CH + 1;
   };
-  auto scan = [&](long long v, long long& all) {
+  long long total = 0, x0 = 0, x1 = 0, ctas;
+  auto shares = [&]() {
+    ctas = min((long long)gridDim.x, total);
+    if (blockIdx.x < ctas) { x0 = share_begin(total, ctas, blockIdx.x); x1 = share_begin(total, ctas, blockIdx.x + 1); }
+  };
+  auto start = [&](int req, const Span& sp, int qb, long long rem) {   // rem: steps of block qb before this CTA's first one
+    Walk<NARROW> W;
+    W.u.req = req; W.u.first = sp.first; W.u.n = sp.n; W.u.len = sp.len; W.u.qb = qb;
+    F::sizes(W.u, group);
+    W.u.h = (int)(rem / W.u.all); W.u.c = (int)(rem - (long long)W.u.h * W.u.all);
+    W.left = x1 - x0; W.seg = 0;
+    s_walk = W;
+  };
+  if (P.n_req <= 8) {
+    // few requests, perhaps of many blocks: every warp by itself, a lane per block
+    Span mine{0, 0, 0};
+    if (lane < P.n_req) mine = request_span(P, lane);
+    for (int pass = 0; pass < 2; ++pass) {
+      long long before = 0;
+      for (int r = 0; r < P.n_req; ++r) {
+        Span sp;
+        sp.first = __shfl_sync(0xffffffffu, mine.first, r); sp.n = __shfl_sync(0xffffffffu, mine.n, r); sp.len = __shfl_sync(0xffffffffu, mine.len, r);
+        const int blocks = F::blocks_of(sp.n, group);
+        for (int b0 = 0; b0 < blocks; b0 += 32) {
+          const int v = b0 + lane < blocks ? unit_steps(sp, b0 + lane) * P.kv_heads : 0;
+          int incl = v;
 #pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-      const long long x = __shfl_up_sync(0xffffffffu, v, o);
-      if (lane >= o) v += x;
+          for (int o = 1; o < 32; o <<= 1) { const int x = __shfl_up_sync(0xffffffffu, incl, o); if (lane >= o) incl += x; }
+          if (pass == 1) {
+            const unsigned here = __ballot_sync(0xffffffffu, x1 > x0 && x0 >= before + incl - v && x0 < before + incl);
+            if (here) {
+              const int src = __ffs(here) - 1;
+              const long long rem = x0 - before - __shfl_sync(0xffffffffu, incl - v, src);
+              if (tid == 0) start(r, sp, b0 + src, rem);
+            }
+          }
+          before += __shfl_sync(0xffffffffu, incl, 31);
+        }
+      }
+      if (pass == 0) { total = before; shares(); }
     }
-    __syncthreads();
-    if (lane == 31) w_sum[warp] = v;
-    __syncthreads();
-    long long before = 0;
-    all = 0;
+  } else {
+    // many: a thread per request
+    auto steps_of = [&](int i) -> long long {
+      const Span sp = request_span(P, i);
+      const int blocks = F::blocks_of(sp.n, group);
+      long long n = 0;
+      for (int qb = 0; qb < blocks; ++qb) n += unit_steps(sp, qb);
+      return n * P.kv_heads;
+    };
+    auto scan = [&](long long v, long long& all) {
 #pragma unroll
-    for (int w = 0; w < AT_THREADS / 32; ++w) { if (w < warp) before += w_sum[w]; all += w_sum[w]; }
-    return v + before;
-  };
-  long long total = 0;
-  for (int base = 0; base < P.n_req; base += AT_THREADS) {
-    long long all;
-    scan(base + tid < P.n_req ? steps_of(base + tid) : 0, all);
-    total += all;
-  }
-  const long long ctas = min((long long)gridDim.x, total);
-  Meta* meta = reinterpret_cast<Meta*>(P.ws) + blockIdx.x;
-  if (blockIdx.x >= ctas) {
-    if (tid == 0) *meta = Meta{};
-    return;
-  }
-  const long long x0 = total * blockIdx.x / ctas, x1 = total * (blockIdx.x + 1) / ctas;
-  {
+      for (int o = 1; o < 32; o <<= 1) {
+        const long long x = __shfl_up_sync(0xffffffffu, v, o);
+        if (lane >= o) v += x;
+      }
+      __syncthreads();
+      if (lane == 31) w_sum[warp] = v;
+      __syncthreads();
+      long long before = 0;
+      all = 0;
+#pragma unroll
+      for (int w = 0; w < AT_THREADS / 32; ++w) { if (w < warp) before += w_sum[w]; all += w_sum[w]; }
+      return v + before;
+    };
+    for (int base = 0; base < P.n_req; base += AT_THREADS) {
+      long long all;
+      scan(base + tid < P.n_req ? steps_of(base + tid) : 0, all);
+      total += all;
+    }
+    shares();
     long long before = 0;
     for (int base = 0; base < P.n_req; base += AT_THREADS) {
       const long long v = base + tid < P.n_req ? steps_of(base + tid) : 0;
       long long all;
       const long long incl = scan(v, all) + before;
-      if (x0 >= incl - v && x0 < incl) {
-        Walk w;
+      if (x1 > x0 && x0 >= incl - v && x0 < incl) {
+        const Span sp = request_span(P, base + tid);
         long long rem = x0 - (incl - v);
-        unit_load(w.u, P, base + tid);
-        for (w.u.qb = 0;; ++w.u.qb) {
-          unit_sizes(w.u, group);
-          if (rem < (long long)w.u.all * P.kv_heads) break;
-          rem -= (long long)w.u.all * P.kv_heads;
+        int qb = 0;
+        for (;; ++qb) {
+          const long long k = (long long)unit_steps(sp, qb) * P.kv_heads;
+          if (rem < k) break;
+          rem -= k;
         }
-        w.u.h = (int)(rem / w.u.all); w.u.c = (int)(rem - (long long)w.u.h * w.u.all);
-        w.left = x1 - x0; w.seg = 0;
-        s_walk = w;
+        start(base + tid, sp, qb, rem);
       }
       before += all;
     }
+  }
+  Meta* meta = reinterpret_cast<Meta*>(P.ws) + blockIdx.x;   // narrow
+  if (x1 == x0) {
+    if (NARROW && tid == 0) *meta = Meta{};
+    return;
   }
   if (warp == 9) tmem_alloc(tmem_slot, 512);
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem = *tmem_slot;
-  Walk W = s_walk;
+  Walk<NARROW>& W = walks[warp];
+  if (lane == 0) W = s_walk;
+  __syncwarp();
+  auto next = [&](int c0, int c1) {                 // on to the next part
+    __syncwarp();
+    if (lane == 0) W.end(P, group, c0, c1);
+    __syncwarp();
+  };
   int c0, c1;
   int fills = 0;                                    // chunks copied (what is in flight is waited for after an abort)
   // where a part's chunks reach past some query's last position
@@ -280,62 +359,79 @@ __global__ void __launch_bounds__(AT_THREADS, 1) k_attend_tc(const __grid_consta
           page = next;
         }
       }
-      W.end(P, group, c0, c1);
+      next(c0, c1);
     }
   } else if (warp == 9) {
     // ------------------------------------------------------------------ MMA issue
     if (lane == 0) {
       const uint32_t idesc_s = instr_desc<BF>(AT_CH, 0), idesc_o = instr_desc<BF>(HD, 1);
-      int it = 0, fix[2] = {0, 0}, pc[2] = {0, 0}, oc[2] = {0, 0};
+      const uint64_t q_desc = desc_sw128(smem_u32(qs), 16, 1024), k_desc = desc_sw128(smem_u32(kst), 16, 1024), v_desc = desc_sw128(smem_u32(vst), AT_CH * 128, 1024);
+      int it = 0, fix[NST] = {}, pc[2] = {0, 0}, oc[2] = {0, 0};
       bool ok = true;
-      auto scores = [&](int t, int i) {              // S of tile t with the chunk in stage i % NST
-        const uint32_t qb = smem_u32(qs) + t * QTILE, kb = smem_u32(kst) + (i % NST) * KBYTES;
+      auto scores = [&](int t, int qt, int i) {      // S of tile t (queries of tile qt) with the chunk in stage i % NST
+        const uint64_t qd = q_desc + (uint64_t)(qt * (QTILE >> 4)), kd = k_desc + (uint64_t)((i % NST) * (KBYTES >> 4));   // (addresses in units of 16 bytes)
 #pragma unroll
         for (int h = 0; h < HALVES; ++h)
 #pragma unroll
-          for (int k = 0; k < 4; ++k)
-            umma_bf16(tmem + t * 128, desc_sw128(qb + h * (128 * 128) + k * 32, 16, 1024), desc_sw128(kb + h * (AT_CH * 128) + k * 32, 16, 1024), idesc_s, (h | k) ? 1u : 0u);
+          for (int k = 0; k < 4; ++k) umma_bf16(tmem + t * 128, qd + h * 1024 + k * 2, kd + h * (AT_CH * 8) + k * 2, idesc_s, (h | k) ? 1u : 0u);
         umma_commit(s_full + t);
+      };
+      auto values = [&](int t, int vs, bool add) {   // O += P.V
+        const uint64_t vd = v_desc + (uint64_t)(vs * (KBYTES >> 4));
+#pragma unroll
+        for (int k = 0; k < AT_CH / 16; ++k) mma_ts(tmem + 256 + t * 128, tmem + t * 128 + k * 8, vd + k * 128, idesc_o, (add || k > 0) ? 1u : 0u);
+      };
+      auto k_wait = [&](int i) { return mbar_wait(k_full + i % NST, (i / NST) & 1, abort_flag, AT_WAIT); };
+      auto p_wait = [&](int t, bool first) {         // tile t's weights are written (and, before a part's first product, its last O has been read)
+        bool r = mbar_wait(p_full + t, pc[t] & 1, abort_flag, AT_WAIT);
+        ++pc[t];
+        if (r && first) { r = mbar_wait(o_free + t, (oc[t] & 1) ^ 1, abort_flag, AT_WAIT); ++oc[t]; }
+        return r;
       };
       while (ok && W.begin(c0, c1)) {
         const Unit& u = W.u;
-        const int n[2] = {max(0, min(c1, u.nch[0]) - c0), max(0, min(c1, u.nch[1]) - c0)}, L = max(n[0], n[1]);
-        const int edge = first_edge(u) - c0;          // chunks from here on are cleaned first
+        const Sh sh(u, c0, c1);
+        const int L = sh.L, edge = first_edge(u) - c0;   // (chunks from `edge` on are cleaned first)
+        auto v_wait = [&](int j) {
+          const int vs = (it + j) % NST;
+          if (j < edge) return mbar_wait(v_full + vs, ((it + j) / NST) & 1, abort_flag, AT_WAIT);
+          const bool r = mbar_wait(v_fixed + vs, fix[vs] & 1, abort_flag, AT_WAIT);
+          ++fix[vs];
+          return r;
+        };
         ok = mbar_wait(q_full, W.seg & 1, abort_flag, AT_WAIT);
         if (ok && L) {
-          ok = mbar_wait(k_full + it % NST, (it / NST) & 1, abort_flag, AT_WAIT);
+          ok = k_wait(it);
           tc_fence_after();
-          if (ok) {
-            if (n[0]) scores(0, it);
-            if (n[1]) scores(1, it);
-            umma_commit(k_empty + it % NST);
-          }
+          if (ok && sh.n[0]) scores(0, 0, it);
+          if (ok && NARROW && L > 1) { ok = k_wait(it + 1); tc_fence_after(); }
+          if (ok && sh.n[1]) scores(1, NARROW ? 0 : 1, NARROW ? it + 1 : it);
         }
-        if (ok && L <= 1) umma_commit(q_empty);
-        for (int j = 0; j < L && ok; ++j) {
-          const int vs = (it + j) % NST;
-          if (j >= edge) { ok = mbar_wait(v_fixed + vs, fix[vs] & 1, abort_flag, AT_WAIT); ++fix[vs]; }
-          else ok = mbar_wait(v_full + vs, ((it + j) / NST) & 1, abort_flag, AT_WAIT);
-          if (ok && j + 1 < L) ok = mbar_wait(k_full + (it + j + 1) % NST, ((it + j + 1) / NST) & 1, abort_flag, AT_WAIT);
-          const uint32_t vb = smem_u32(vst) + vs * KBYTES;
-#pragma unroll
-          for (int t = 0; t < 2; ++t) {
-            if (!ok || j >= n[t]) continue;
-            ok = mbar_wait(p_full + t, pc[t] & 1, abort_flag, AT_WAIT);
-            ++pc[t];
-            if (ok && j == 0) { ok = mbar_wait(o_free + t, (oc[t] & 1) ^ 1, abort_flag, AT_WAIT); ++oc[t]; }   // (the last part's O has been read)
-            if (!ok) continue;
+        if (ok && L <= (NARROW ? 2 : 1)) umma_commit(q_empty);
+        if (NARROW) {
+          for (int j = 0; j < L && ok; ++j) {
+            const int t = j & 1;
+            ok = v_wait(j) && p_wait(t, j < 2) && (j + 2 >= L || k_wait(it + j + 2));
+            if (!ok) break;
             tc_fence_after();
-#pragma unroll
-            for (int k = 0; k < AT_CH / 16; ++k)
-              mma_ts(tmem + 256 + t * 128, tmem + t * 128 + k * 8, desc_sw128(vb + k * 2048, AT_CH * 128, 1024), idesc_o, (j > 0 || k > 0) ? 1u : 0u);
-            if (j + 1 < n[t]) scores(t, it + j + 1);
-            else umma_commit(o_full + t);
+            values(t, (it + j) % NST, j >= 2);
+            if (j + 2 < L) scores(t, 0, it + j + 2); else umma_commit(o_full + t);
+            if (j + 3 == L) umma_commit(q_empty);
           }
-          if (!ok) break;
-          umma_commit(v_empty + vs);
-          if (j + 1 < L) umma_commit(k_empty + (it + j + 1) % NST);
-          if (j + 2 == L) umma_commit(q_empty);
+        } else {
+          for (int j = 0; j < L && ok; ++j) {
+            ok = v_wait(j) && (j + 1 >= L || k_wait(it + j + 1));
+#pragma unroll
+            for (int t = 0; t < 2; ++t) {
+              if (!ok || j >= sh.n[t]) continue;
+              ok = p_wait(t, j == 0);
+              if (!ok) continue;
+              tc_fence_after();
+              values(t, (it + j) % NST, j > 0);
+              if (j + 1 < sh.n[t]) scores(t, t, it + j + 1); else umma_commit(o_full + t);
+            }
+            if (ok && j + 2 == L) umma_commit(q_empty);
+          }
         }
         it += L;
         W.end(P, group, c0, c1);
@@ -352,19 +448,21 @@ __global__ void __launch_bounds__(AT_THREADS, 1) k_attend_tc(const __grid_consta
       ok = __all_sync(0xffffffffu, mbar_wait(q_empty, (W.seg & 1) ^ 1, abort_flag, AT_WAIT));
       if (!ok) break;
       constexpr int PC = HD / 8;
+      const Sh sh(u, c0, c1);
+#pragma unroll 4
       for (int i = ft; i < AT_ROWS * PC; i += 64) {
         const int r = i / PC, c = i % PC, qi = u.qb * AT_ROWS + r, j = qi / group;
         const bool on = j < u.n && c < pieces;
         const T* src = reinterpret_cast<const T*>(P.q) + (on ? (u.first + j) * P.q_row + (u.h * group + qi - j * group) * P.q_head + c * 8 : 0);
         const uint32_t dst = smem_u32(qs) + (r >> 7) * QTILE + (c >> 3) * (128 * 128) + (r & 127) * 128 + (((c & 7) ^ (r & 7)) << 4);
-        asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(on ? 16 : 0) : "memory");
+        asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(on ? 16 : 0));
       }
       asm volatile("cp.async.commit_group;\n\tcp.async.wait_group 0;" ::: "memory");
       asm volatile("fence.proxy.async.shared::cta;" ::: "memory");   // the tensor core reads these tiles through the async proxy
       __syncwarp();
       if (lane == 0) mbar_arrive(q_full);
-      const int L = max(max(0, min(c1, u.nch[0]) - c0), min(c1, u.nch[1]) - c0), edge = first_edge(u) - c0;
-      volatile int* odd_flag = odd_ring + W.seg % AT_RING * 2 + warp - 10;
+      const int L = sh.L, edge = first_edge(u) - c0;
+      volatile int* odd_flag = odd_ring + W.seg % AT_PARTS * 2 + warp - 10;
       if (lane == 0) *odd_flag = 0;
       __syncwarp();
       for (int j = max(edge, 0); j < L && ok; ++j) {
@@ -395,52 +493,67 @@ __global__ void __launch_bounds__(AT_THREADS, 1) k_attend_tc(const __grid_consta
         if (lane == 0) mbar_arrive(v_fixed + s);
       }
       it += L;
-      W.end(P, group, c0, c1);
+      next(c0, c1);
     }
   } else {
     // ------------------------------------------------------------------ softmax: one thread per query
     const int t = warp >> 2, quad = warp & 3, ql = quad * 32 + lane;
     const uint32_t sel = (uint32_t)(quad * 32) << 16, ts = tmem + t * 128 + sel, to = tmem + 256 + t * 128 + sel;
     const float sc = P.scale * 1.4426950408889634f;   // (> 0: maxima are taken of the unscaled scores)
-    int sn = 0, on = 0, it = 0;
+    int sn = 0, on = 0, xn = 0, it = 0;
     bool ok = true;
     auto wait = [&](uint64_t* bar, uint32_t parity) { return (bool)__all_sync(0xffffffffu, mbar_wait(bar, parity, abort_flag, AT_WAIT)); };
     while (ok && W.begin(c0, c1)) {
       const Unit& u = W.u;
-      const int n_t = max(0, min(c1, u.nch[t]) - c0), L = max(max(0, min(c1, u.nch[0]) - c0), min(c1, u.nch[1]) - c0);
-      const int qi = u.qb * AT_ROWS + t * 128 + ql, jr = qi / group;
+      const Sh sh(u, c0, c1);
+      const int n_t = sh.n[t], L = sh.L, row = NARROW ? ql : t * 128 + ql;                       // row: of the unit's queries
+      const int stride = NARROW ? 2 : 1, first_j = NARROW ? t : 0;
+      const bool returns = NARROW || t == (sh.n[1] > 0);                                        // this tile's products are the last ones on a chunk
+      const int qi = u.qb * AT_ROWS + row, jr = qi / group;
       const bool mine = jr < u.n;
       const int last = mine ? u.len - u.n + jr : -1;                                             // last position that this query sees
-      const int warp_first = u.len - u.n + (u.qb * AT_ROWS + t * 128 + quad * 32) / group;
-      const bool idle = u.qb * AT_ROWS + t * 128 + quad * 32 >= u.n * group;                     // no query in this warp: its rows hold anything
+      const int warp_first = u.len - u.n + (qi - lane) / group;
+      const bool idle = qi - lane >= u.n * group;                                                // no query in this warp: its rows hold anything
       float m_run = -INFINITY, l_run = 0.f;
-      for (int j = 0; j < n_t && ok; ++j) {
+      for (int i = 0; i < n_t && ok; ++i) {
+        const int j = first_j + i * stride;
         ok = wait(s_full + t, sn & 1);
         ++sn;
         if (!ok) break;
+        if (returns && quad == 0 && lane == 0) {      // the scores are done with K, and the products before them with V
+          mbar_arrive(k_empty + (it + j) % NST);
+          if (i > 0) mbar_arrive(v_empty + (it + j - stride) % NST);
+        }
         if (idle) {
           if (lane == 0) mbar_arrive(p_full + t);
           continue;
         }
         tc_fence_after();
-        uint32_t sr[AT_CH];
-#pragma unroll
-        for (int x = 0; x < AT_CH; x += 32) ld32(ts + x, sr + x);
-        ld_wait<AT_CH>(sr);
         const int p0 = (c0 + j) * AT_CH;
         const unsigned valid = valid_ring[(it + j) % AT_RING];
-        if (p0 + AT_CH - 1 > warp_first || valid != 0xffffffffu) {
-          const int shift = 31 - __clz(J.box_rows);
+        const bool edge = p0 + AT_CH - 1 > warp_first || valid != 0xffffffffu;
+        // 64 scores of a row at a time, read twice: for the maximum, and for the weights (a whole row in registers spills; TMEM reads are
+        // quick).  Positions that the query does not see: -infinity.
+        uint32_t sr[64];
+        auto half_row = [&](int h) {
+          ld32(ts + h * 64, sr);
+          ld32(ts + h * 64 + 32, sr + 32);
+          ld_wait<64>(sr);
+          if (edge) {
+            const int shift = 31 - __clz(J.box_rows);
 #pragma unroll
-          for (int x = 0; x < AT_CH; ++x) if (p0 + x > last || !((valid >> (x >> shift)) & 1u)) sr[x] = 0xff800000u;   // -inf
+            for (int x = 0; x < 64; ++x) if (p0 + h * 64 + x > last || !((valid >> ((h * 64 + x) >> shift)) & 1u)) sr[x] = 0xff800000u;
+          }
+        };
+        float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+        for (int h = 0; h < AT_CH / 64; ++h) {
+          half_row(h);
+#pragma unroll
+          for (int x = 0; x < 64; x += 8)
+#pragma unroll
+            for (int y = 0; y < 4; ++y) mx[y] = fmaxf(fmaxf(mx[y], __uint_as_float(sr[x + y])), __uint_as_float(sr[x + y + 4]));
         }
-        float mx[4];
-#pragma unroll
-        for (int x = 0; x < 4; ++x) mx[x] = fmaxf(__uint_as_float(sr[x]), __uint_as_float(sr[x + 4]));
-#pragma unroll
-        for (int x = 8; x < AT_CH; x += 8)
-#pragma unroll
-          for (int y = 0; y < 4; ++y) mx[y] = fmaxf(fmaxf(mx[y], __uint_as_float(sr[x + y])), __uint_as_float(sr[x + y + 4]));
         const float seen = fmaxf(m_run, fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * sc);
         // The reference follows the running maximum only when that has moved by more than 2^8: weights of up to 256 are as exact, and
         // O is rescaled a few times a row instead of every chunk.
@@ -449,7 +562,7 @@ __global__ void __launch_bounds__(AT_THREADS, 1) k_attend_tc(const __grid_consta
         const float corr = ex2a(m_run - off);
         const float2 s2 = make_float2(sc, sc), o2 = make_float2(-off, -off);
         float2 sum[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
-        if (j > 0 && __any_sync(0xffffffffu, corr != 1.0f)) {   // (the scores' completion is also that of the products before them)
+        if (i > 0 && __any_sync(0xffffffffu, corr != 1.0f)) {   // (the scores' completion is also that of the products before them)
 #pragma unroll 1
           for (int d = 0; d < HD; d += 32) {
             uint32_t v[32];
@@ -461,14 +574,17 @@ __global__ void __launch_bounds__(AT_THREADS, 1) k_attend_tc(const __grid_consta
           }
         }
 #pragma unroll
-        for (int x = 0; x < AT_CH; x += 2) {
-          float2 e = fma2(make_float2(__uint_as_float(sr[x]), __uint_as_float(sr[x + 1])), s2, o2);
-          e.x = ex2a(e.x); e.y = ex2a(e.y);
-          sum[(x >> 1) & 1] = add2(sum[(x >> 1) & 1], e);
-          sr[x / 2] = pack2<T>(e.x, e.y);
+        for (int h = 0; h < AT_CH / 64; ++h) {
+          half_row(h);
+#pragma unroll
+          for (int x = 0; x < 64; x += 2) {
+            float2 e = fma2(make_float2(__uint_as_float(sr[x]), __uint_as_float(sr[x + 1])), s2, o2);
+            e.x = ex2a(e.x); e.y = ex2a(e.y);
+            sum[(x >> 1) & 1] = add2(sum[(x >> 1) & 1], e);
+            sr[x / 2] = pack2<T>(e.x, e.y);
+          }
+          st32(ts + h * 32, sr);                     // (over scores that have been read twice)
         }
-        st32(ts, sr);
-        st32(ts + 32, sr + 32);
         sum[0] = add2(sum[0], sum[1]);
         l_run = l_run * corr + (sum[0].x + sum[0].y);
         m_run = m_new;
@@ -478,21 +594,105 @@ __global__ void __launch_bounds__(AT_THREADS, 1) k_attend_tc(const __grid_consta
         if (lane == 0) mbar_arrive(p_full + t);
       }
       if (!ok) break;
-      const bool cut = c0 > 0 || c1 < u.all;
-      float* part = reinterpret_cast<float*>(reinterpret_cast<unsigned char*>(P.ws) + (size_t)gridDim.x * sizeof(Meta)) +
-                    (size_t)(2 * blockIdx.x + (W.seg ? 1 : 0)) * (AT_ROWS * (P.hd + 2));
-      const int row = t * 128 + ql;
-      T* dst = reinterpret_cast<T*>(P.o) + (u.first + jr) * P.o_row + (u.h * group + qi - jr * group) * P.o_head;
-      const float inv = m_run == -INFINITY ? 0.f : 1.f / l_run;
+      const bool is_cut = c0 > 0 || c1 < u.all;
+      const size_t slot_floats = (size_t)AT_ROWS * (P.hd + 2);                                   // [column / 4][row][4], then maxima and sums
+      float* parts = NARROW ? const_cast<float*>(parts_of(P, gridDim.x)) : reinterpret_cast<float*>(P.ws) + (size_t)gridDim.x * 8;
+      const int own_slot = 2 * blockIdx.x + (W.seg ? 1 : 0);
+      Cut cut{};
+      if (is_cut) { const long long u0 = x1 - W.left - c0; cut = cut_of(u0, u0 + u.all, total, ctas); }
+      unsigned* count = reinterpret_cast<unsigned*>(P.ws) + cut.owner * 8 + (NARROW ? quad : warp);   // of the parts of these 32 queries
       if (n_t) {
         ok = wait(o_full + t, on & 1);
         ++on;
         if (!ok) break;
+        if (returns && quad == 0 && lane == 0) mbar_arrive(v_empty + (it + first_j + (n_t - 1) * stride) % NST);
         tc_fence_after();
       }
-      const bool odd = odd_ring[W.seg % AT_RING * 2] | odd_ring[W.seg % AT_RING * 2 + 1];
+      const bool odd = odd_ring[W.seg % AT_PARTS * 2] | odd_ring[W.seg % AT_PARTS * 2 + 1];
+      const bool give = NARROW && t == 1, take = NARROW && t == 0 && sh.n[1] > 0;
+      float f_own = 1.f, f_other = 0.f;
+      if (give && n_t) { other_ml[ql] = m_run; other_ml[128 + ql] = l_run; }   // (read with the first columns; the last part's were read before its last columns were)
+      float* tile = xch + (NARROW ? quad : warp) * (32 * 20);            // 32 rows x 16 columns on their way to whole sectors
+      const bool put = !give && !idle;
+      // last: the other parts are all there (or this one is all), so this one need not be filed
+      bool last_part = !is_cut;
+      if (NARROW && is_cut && tid == 0 && cut.owner == (int)blockIdx.x) s_meta = Meta{cut, u.first, u.n, u.qb, u.h, 0};
+      if (!NARROW && is_cut && put) {
+        unsigned n = 0;
+        if (lane == 0) asm volatile("ld.acquire.gpu.global.u32 %0, [%1];" : "=r"(n) : "l"(count) : "memory");
+        last_part = __shfl_sync(0xffffffffu, n, 0) == (unsigned)cut.parts - 1;
+        if (last_part) __threadfence();
+        __syncwarp();
+      }
+      // one row's values of the other parts (own_too: of all), added to v; `scale` of the own ones
+      float M = m_run, lsum = l_run, own = 1.f;
+      auto others_ml = [&](bool own_too) {
+#pragma unroll 4
+        for (int p = 0; p < cut.parts; ++p)
+          if (own_too || cut.slot(p) != own_slot) M = fmaxf(M, __ldcg(parts + cut.slot(p) * slot_floats + (size_t)AT_ROWS * P.hd + row));
+        own = m_run == -INFINITY ? 0.f : ex2a(m_run - M);
+        lsum = own == 0.f ? 0.f : l_run * own;
+#pragma unroll 4
+        for (int p = 0; p < cut.parts; ++p)
+          if (own_too || cut.slot(p) != own_slot) {
+            const float* s = parts + cut.slot(p) * slot_floats + (size_t)AT_ROWS * P.hd + row;
+            const float mp = __ldcg(s), lp = __ldcg(s + AT_ROWS), w = mp == -INFINITY ? 0.f : ex2a(mp - M);
+            if (w != 0.f) lsum = fmaf(lp, w, lsum);
+          }
+      };
+      auto add_others = [&](uint32_t* v, int d, bool own_too) {
+#pragma unroll
+        for (int x = 0; x < 32; ++x) v[x] = own == 0.f ? 0u : __float_as_uint(__uint_as_float(v[x]) * own);
 #pragma unroll 1
-      for (int d = 0; d < HD && !idle; d += 32) {
+        for (int p0 = 0; p0 < cut.parts; p0 += 3) {    // three parts' loads under way together
+          float w[3];
+          float4 y[3][8];
+#pragma unroll
+          for (int k = 0; k < 3; ++k) {
+            const int p = p0 + k;
+            const bool on = p < cut.parts && (own_too || cut.slot(p) != own_slot);
+            const float* s = parts + cut.slot(on ? p : 0) * slot_floats;
+            const float mp = on ? __ldcg(s + (size_t)AT_ROWS * P.hd + row) : -INFINITY;
+            w[k] = mp == -INFINITY ? 0.f : ex2a(mp - M);
+#pragma unroll
+            for (int x = 0; x < 8; ++x) y[k][x] = on && d + 4 * x < P.hd ? __ldcg(reinterpret_cast<const float4*>(s + ((size_t)(d / 4 + x) * AT_ROWS + row) * 4)) : make_float4(0.f, 0.f, 0.f, 0.f);
+          }
+#pragma unroll
+          for (int k = 0; k < 3; ++k) {
+            if (w[k] == 0.f) continue;
+#pragma unroll
+            for (int x = 0; x < 8; ++x) {
+              v[4 * x] = __float_as_uint(fmaf(y[k][x].x, w[k], __uint_as_float(v[4 * x]))); v[4 * x + 1] = __float_as_uint(fmaf(y[k][x].y, w[k], __uint_as_float(v[4 * x + 1])));
+              v[4 * x + 2] = __float_as_uint(fmaf(y[k][x].z, w[k], __uint_as_float(v[4 * x + 2]))); v[4 * x + 3] = __float_as_uint(fmaf(y[k][x].w, w[k], __uint_as_float(v[4 * x + 3])));
+            }
+          }
+        }
+      };
+      auto store = [&](uint32_t* v, int d) {           // a row a thread -> two lanes a row: stores of whole 32-byte sectors
+#pragma unroll
+        for (int g = 0; g < 2; ++g) {
+          __syncwarp();
+#pragma unroll
+          for (int x = 0; x < 16; x += 4) *reinterpret_cast<uint4*>(tile + lane * 20 + x) = make_uint4(v[g * 16 + x], v[g * 16 + x + 1], v[g * 16 + x + 2], v[g * 16 + x + 3]);
+          tile[lane * 20 + 16] = M == -INFINITY ? 0.f : 1.f / lsum;
+          __syncwarp();
+#pragma unroll
+          for (int k = 0; k < 2; ++k) {
+            const int r = k * 16 + (lane >> 1), c = (lane & 1) * 8, dc = d + g * 16 + c, q2 = qi - lane + r;
+            if (q2 < u.n * group && dc < P.hd) {
+              const float* s = tile + r * 20 + c;
+              const float k2 = tile[r * 20 + 16];
+              uint4 w;
+              w.x = pack2<T>(s[0] * k2, s[1] * k2); w.y = pack2<T>(s[2] * k2, s[3] * k2);
+              w.z = pack2<T>(s[4] * k2, s[5] * k2); w.w = pack2<T>(s[6] * k2, s[7] * k2);
+              const int j2 = q2 / group;
+              *reinterpret_cast<uint4*>(reinterpret_cast<T*>(P.o) + (u.first + j2) * P.o_row + (u.h * group + q2 - j2 * group) * P.o_head + dc) = w;
+            }
+          }
+        }
+      };
+#pragma unroll 1
+      for (int d = 0; d < HD && ok && (give || take || put) && (n_t || put); d += 32) {
         uint32_t v[32];
         __syncwarp();
         if (n_t) { ld32(to + d, v); ld_wait<32>(v); }
@@ -500,8 +700,42 @@ __global__ void __launch_bounds__(AT_THREADS, 1) k_attend_tc(const __grid_consta
 #pragma unroll
           for (int x = 0; x < 32; ++x) v[x] = 0u;
         }
-        if (!mine) continue;
-        if (odd) {                                    // infinities and NaN that were taken out, of positions that this query sees
+        if (give) {
+          ok = wait(x_free, (xn & 1) ^ 1);
+          ++xn;
+          if (!ok) break;
+#pragma unroll
+          for (int x = 0; x < 32; x += 4) *reinterpret_cast<uint4*>(other + ql * 36 + x) = make_uint4(v[x], v[x + 1], v[x + 2], v[x + 3]);
+          __syncwarp();
+          if (lane == 0) mbar_arrive(x_full);
+          continue;
+        }
+        if (take) {
+          ok = wait(x_full, xn & 1);
+          ++xn;
+          if (!ok) break;
+          if (d == 0) {
+            const float m2 = other_ml[ql], l2 = other_ml[128 + ql], m = fmaxf(m_run, m2), ref = m == -INFINITY ? 0.f : m;
+            f_own = m_run == -INFINITY ? 0.f : ex2a(m_run - ref);
+            f_other = m2 == -INFINITY ? 0.f : ex2a(m2 - ref);
+            l_run = (f_own == 0.f ? 0.f : l_run * f_own) + (f_other == 0.f ? 0.f : l2 * f_other);
+            m_run = m;
+            M = m; lsum = l_run;
+          }
+#pragma unroll
+          for (int x = 0; x < 32; x += 4) {
+            const float4 w = *reinterpret_cast<const float4*>(other + ql * 36 + x);
+            const float ws[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+            for (int z = 0; z < 4; ++z)
+              v[x + z] = __float_as_uint((f_own == 0.f ? 0.f : __uint_as_float(v[x + z]) * f_own) + (f_other == 0.f ? 0.f : ws[z] * f_other));
+          }
+          __syncwarp();
+          if (lane == 0) mbar_arrive(x_free);
+        }
+        if (!put) continue;
+        if (odd && mine) {                             // infinities and NaN that were taken out, of positions that this query sees
+#pragma unroll 1
           for (int p = max(first_edge(u), c0) * AT_CH; p <= min(last, c1 * AT_CH - 1); ++p) {
             const int b = p / P.page_tokens, page = P.table[(size_t)u.req * P.max_blocks + b];
             if (page < 0 || page >= P.n_pages) continue;
@@ -516,29 +750,49 @@ __global__ void __launch_bounds__(AT_THREADS, 1) k_attend_tc(const __grid_consta
             }
           }
         }
-        if (cut) {
+        if (!last_part) {
 #pragma unroll
           for (int x = 0; x < 32; x += 4)
-            if (d + x < P.hd) *reinterpret_cast<uint4*>(part + (size_t)row * P.hd + d + x) = make_uint4(v[x], v[x + 1], v[x + 2], v[x + 3]);
-        } else {
+            if (d + x < P.hd) *reinterpret_cast<uint4*>(parts + own_slot * slot_floats + ((size_t)(d + x) / 4 * AT_ROWS + row) * 4) = make_uint4(v[x], v[x + 1], v[x + 2], v[x + 3]);
+          continue;
+        }
+        if (!NARROW && is_cut) {
+          if (d == 0) others_ml(false);
+          add_others(v, d, false);
+        }
+        store(v, d);
+      }
+      if (put && !last_part && ok) {
+        parts[own_slot * slot_floats + (size_t)AT_ROWS * P.hd + row] = m_run;
+        parts[own_slot * slot_floats + (size_t)AT_ROWS * (P.hd + 1) + row] = l_run;
+        unsigned n = 0;
+        if (!NARROW) {
+          __threadfence();
+          __syncwarp();
+          if (lane == 0) n = atomicAdd(count, 1u);
+        }
+        if (!NARROW && __shfl_sync(0xffffffffu, n, 0) == (unsigned)cut.parts - 1) {   // (the others came in the meantime)
+          __threadfence();
+          m_run = M = -INFINITY; l_run = 0.f;
+          others_ml(true);
+#pragma unroll 1
+          for (int d = 0; d < HD; d += 32) {
+            uint32_t v[32];
 #pragma unroll
-          for (int x = 0; x < 32; x += 8)
-            if (d + x < P.hd) {
-              uint4 w;
-              w.x = pack2<T>(__uint_as_float(v[x]) * inv, __uint_as_float(v[x + 1]) * inv); w.y = pack2<T>(__uint_as_float(v[x + 2]) * inv, __uint_as_float(v[x + 3]) * inv);
-              w.z = pack2<T>(__uint_as_float(v[x + 4]) * inv, __uint_as_float(v[x + 5]) * inv); w.w = pack2<T>(__uint_as_float(v[x + 6]) * inv, __uint_as_float(v[x + 7]) * inv);
-              *reinterpret_cast<uint4*>(dst + d + x) = w;
-            }
+            for (int x = 0; x < 32; ++x) v[x] = 0u;
+            add_others(v, d, true);
+            store(v, d);
+          }
         }
       }
-      if (cut && mine) { part[(size_t)AT_ROWS * P.hd + row] = m_run; part[(size_t)AT_ROWS * (P.hd + 1) + row] = l_run; }
+      if (!ok) break;
       if (n_t) {
         tc_fence_before();
         __syncwarp();
         if (lane == 0) mbar_arrive(o_free + t);
       }
       it += L;
-      W.end(P, group, c0, c1);
+      next(c0, c1);
     }
   }
   // ------------------------------------------------------------------ teardown
@@ -555,38 +809,44 @@ __global__ void __launch_bounds__(AT_THREADS, 1) k_attend_tc(const __grid_consta
     }
     __syncthreads();
   }
-  if (tid == 0) {
-    // the unit that goes on in the next CTAs, if one begins here and does not end
-    Walk w = s_walk;
-    Meta m{};
-    m.failed = *abort_flag;
+  if (*abort_flag && warp < 8) {
+    // a wait ran out (which takes a broken device): what this CTA had to compute says so
+    Walk<NARROW> w = s_walk;
     int a, b;
     while (w.begin(a, b)) {
-      if (a == 0 && b < w.u.all) {
-        const long long end = x1 + (w.u.all - b);               // one past the unit's last step
-        long long e = (end * ctas - 1) / total;                 // the CTA whose part holds that step (about; corrected below)
-        while (e > 0 && total * e / ctas >= end) --e;
-        while (total * (e + 1) / ctas < end) ++e;
-        m.parts = (int)(e - blockIdx.x) + 1;
-        m.slot = 2 * blockIdx.x + (w.seg ? 1 : 0); m.first = w.u.first; m.n = w.u.n; m.qb = w.u.qb; m.h = w.u.h;
+      for (int r = tid; r < AT_ROWS; r += 256) {
+        const int q = w.u.qb * AT_ROWS + r, j = q / group;
+        if (j >= w.u.n) continue;
+        T* dst = reinterpret_cast<T*>(P.o) + (w.u.first + j) * P.o_row + (w.u.h * group + q - j * group) * P.o_head;
+        for (int d = 0; d < P.hd; ++d) dst[d] = from_f32<T>(NAN);
       }
       w.end(P, group, a, b);
     }
-    *meta = m;
   }
   if (warp == 9) { tc_fence_after(); tmem_dealloc(tmem, 512); }
+  if (NARROW && tid == 0) {
+    s_meta.failed = *abort_flag;
+    *meta = s_meta;
+  }
 }
 
 typedef CUresult (*EncodeFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*, const cuuint32_t*, const cuuint32_t*,
                              CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
 
-template <typename T, int HD> int launch(const TcParams& J, cudaStream_t st) {
-  auto kern = k_attend_tc<T, HD>;
+template <typename T, int HD, bool NARROW> int launch(const TcParams& J, cudaStream_t st) {
+  auto kern = k_attend_tc<T, HD, NARROW>;
+  static_assert(at_smem<HD, NARROW>() <= 225 * 1024, "shared memory");
   static std::atomic<unsigned long long> done{0};
-  if (int rc = allow_shared(done, reinterpret_cast<const void*>(kern), at_smem<HD>())) return rc;
-  kern<<<AM_SMS, AT_THREADS, at_smem<HD>(), st>>>(J);
+  if (int rc = allow_shared(done, reinterpret_cast<const void*>(kern), at_smem<HD, NARROW>())) return rc;
+  if (!NARROW) SCK(cudaMemsetAsync(J.a.ws, 0, (size_t)AM_SMS * 32, st));   // the counts of parts, for 32 queries each
+  kern<<<AM_SMS, AT_THREADS, at_smem<HD, NARROW>(), st>>>(J);
   SCK(cudaGetLastError());
-  return launch_join<T, AT_ROWS, true>(J.a, AM_SMS, 8, st);
+  if constexpr (NARROW) return launch_join<T, Form<true>::ROWS, true>(J.a, AM_SMS, st);
+  return STAIRS_OK;
+}
+template <typename T> int launch_form(const TcParams& J, bool narrow, cudaStream_t st) {
+  if (J.a.hd <= 64) return narrow ? launch<T, 64, true>(J, st) : launch<T, 64, false>(J, st);
+  return narrow ? launch<T, 128, true>(J, st) : launch<T, 128, false>(J, st);
 }
 
 }  // namespace
@@ -595,11 +855,12 @@ template <typename T, int HD> int launch(const TcParams& J, cudaStream_t st) {
 bool tc_takes(const stairs_paged* c, float scale) {
   const int p = c->page_tokens;
   auto stride = [](int64_t s, int n) { return n == 1 || (s > 0 && s < (1ll << 39)); };
-  return c->head_dim <= 128 && (p % AT_CH == 0 || (p >= 8 && p < AT_CH && (p & (p - 1)) == 0)) && scale > 0.f && stride(c->token_stride, 2) &&
+  return c->head_dim <= 128 && (p % 128 == 0 || (p >= 8 && p < 128 && (p & (p - 1)) == 0)) && scale > 0.f && stride(c->token_stride, 2) &&
          stride(c->head_stride, c->n_kv_heads) && stride(c->page_stride, c->n_pages);
 }
 
-size_t tc_workspace(int hd) { return (size_t)AM_SMS * (sizeof(Meta) + (size_t)2 * AT_ROWS * (hd + 2) * 4); }
+// two parts a CTA, of 128 or 256 rows
+size_t tc_workspace(int hd) { return (size_t)AM_SMS * (64 + (size_t)2 * 256 * (hd + 2) * 4) + 256; }
 
 int launch_tc(const AttendParams& P, int dtype, cudaStream_t st) {
   static EncodeFn encode = nullptr;              // (the driver's function: the same whoever looks it up)
@@ -612,7 +873,12 @@ int launch_tc(const AttendParams& P, int dtype, cudaStream_t st) {
   }
   TcParams J;
   J.a = P;
-  J.box_rows = P.page_tokens < AT_CH ? P.page_tokens : AT_CH;
+  // units of 128 queries where the average request has no more, and where units of 256 would be few: each would be cut into many parts, which its
+  // last warp reads one by one (one request, 256 queries a key head after 16384 tokens: wide 169 us)
+  const long long q = (long long)P.n_rows * (P.heads / P.kv_heads), wide_units = (q + 255) / 256 * P.kv_heads;
+  const bool narrow = q <= 128ll * P.n_req || wide_units < AM_SMS / 2;
+  const int ch = narrow ? Form<true>::CH : Form<false>::CH;
+  J.box_rows = P.page_tokens < ch ? P.page_tokens : ch;
   // the coordinates between the elements and the pages: the one of the smaller stride first
   J.heads_outer = P.kv_heads > 1 && P.head_stride > P.token_stride;
   const cuuint64_t tok = (cuuint64_t)P.token_stride * 2, head = (cuuint64_t)(P.kv_heads > 1 ? P.head_stride : P.token_stride) * 2;   // (one head: any stride)
@@ -623,8 +889,7 @@ int launch_tc(const AttendParams& P, int dtype, cudaStream_t st) {
     if (encode(v ? &J.vmap : &J.kmap, dtype == DT_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 4, const_cast<void*>(v ? P.vc : P.kc), dims, strides, box,
                es, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
       return static_fail(STAIRS_ECUDA, "stairs_attend_static: cuTensorMapEncodeTiled failed for the cache");
-  if (P.hd <= 64) return dtype == DT_BF16 ? launch<bf16, 64>(J, st) : launch<__half, 64>(J, st);
-  return dtype == DT_BF16 ? launch<bf16, 128>(J, st) : launch<__half, 128>(J, st);
+  return dtype == DT_BF16 ? launch_form<bf16>(J, narrow, st) : launch_form<__half>(J, narrow, st);
 }
 
 }  // namespace att

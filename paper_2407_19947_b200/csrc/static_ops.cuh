@@ -18,15 +18,18 @@ int static_fail(int code, const char* fmt, ...);
                                  __FILE__, __LINE__);                                                   \
   } while (0)
 
-// Lets `kern` have `bytes` of shared memory, once per device (the call takes the host about a microsecond).
-inline int allow_shared(std::atomic<unsigned long long>& done, const void* kern, int bytes) {
+// Sets an attribute of a kernel once per device (the call takes the host about a microsecond).
+inline int allow_once(std::atomic<unsigned long long>& done, const void* kern, cudaFuncAttribute what, int value) {
   int dev = 0;
   SCK(cudaGetDevice(&dev));
   const unsigned long long bit = 1ull << (dev & 63);
   if (dev < 64 && (done.load(std::memory_order_relaxed) & bit)) return STAIRS_OK;
-  SCK(cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes));
+  SCK(cudaFuncSetAttribute(kern, what, value));
   if (dev < 64) done.fetch_or(bit, std::memory_order_relaxed);
   return STAIRS_OK;
+}
+inline int allow_shared(std::atomic<unsigned long long>& done, const void* kern, int bytes) {
+  return allow_once(done, kern, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
 }
 
 enum Dtype { DT_F32 = 0, DT_BF16 = 1, DT_F16 = 2 };

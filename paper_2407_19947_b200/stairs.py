@@ -114,7 +114,7 @@ def load_library(path: Optional[str] = None):
     lib.stairs_tables_static.argtypes = [C.c_int, vp, vp, vp, vp, C.c_int, C.c_int, vp, C.c_int, vp, C.c_int] + [vp] * 9
     lib.stairs_append_static.argtypes = [vp, C.c_int, vp, vp, C.c_int, C.c_int64, C.c_int64, vp, vp]
     lib.stairs_attend_workspace_bytes.restype = C.c_size_t
-    lib.stairs_attend_workspace_bytes.argtypes = [C.POINTER(CPaged), C.c_int, C.c_int, C.c_int]
+    lib.stairs_attend_workspace_bytes.argtypes = [C.POINTER(CPaged), C.c_int, C.c_int, C.c_int, C.c_int]
     lib.stairs_attend_static.argtypes = [vp, vp, C.c_int, C.c_int, vp, vp, C.c_int, C.c_int, C.c_int, vp, C.c_int64,
                                          C.c_int64, C.c_float, vp, C.c_int64, C.c_int64, vp, C.c_size_t, vp]
     lib.stairs_sample_static.argtypes = [vp, C.c_int, C.c_int, C.c_int64, C.c_int, i32p, vp, vp, vp, C.c_int, vp, vp, vp]
@@ -496,10 +496,10 @@ def append_static(k_new, v_new, k_cache, v_cache, row_slot) -> None:
 
 
 @functools.lru_cache(maxsize=1024)
-def _attend_scratch(page_tokens, kv_heads, head_dim, code, heads, n_req, rows):
+def _attend_scratch(page_tokens, kv_heads, head_dim, code, heads, n_req, rows, max_len):
     """Bytes that a call of these sizes asks for (a cache of any length and strides)."""
     c = CPaged(4096, 4096, 4096, 4096, 4096, 2, page_tokens, kv_heads, head_dim, code)   # (addresses and strides that every form of the kernels takes)
-    return load_library().stairs_attend_workspace_bytes(C.byref(c), heads, n_req, rows)
+    return load_library().stairs_attend_workspace_bytes(C.byref(c), heads, n_req, rows, max_len)
 
 
 @_on_stream
@@ -525,7 +525,10 @@ def attend_static(q, k_cache, v_cache, block_table, row_off, kv_len, *, scale: O
         out = q.new_empty(shape)
     elif out.shape != shape or out.dtype != q.dtype or (hd != 1 and out.stride(2) != 1):
         _refuse("out has to be like q")
-    need = _attend_scratch(k_cache.shape[1], kv_heads, hd, _DTYPES[q.dtype], heads, n, rows) if rows else 0
+    reach = bt[1] * k_cache.shape[1]
+    if not 0 < max_len < reach:
+        max_len = max_len if max_len < 0 else reach
+    need = _attend_scratch(k_cache.shape[1], kv_heads, hd, _DTYPES[q.dtype], heads, n, rows, max_len) if rows else 0
     ws = q.new_empty(need, dtype=torch.uint8) if need else None
     so = out.stride()
     _call(dev, lib.stairs_attend_static, c, block_table.data_ptr(), bt[1], n, row_off.data_ptr(), kv_len.data_ptr(), max_len, rows, heads, q.data_ptr(),

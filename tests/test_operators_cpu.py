@@ -75,7 +75,7 @@ def test_calls_of_no_rows_enqueue_nothing(lib):
     assert attend(lib, rows=0, q=None, o=None) == 0
     c = cache()
     assert lib.stairs_append_static(C.byref(c), 0, None, None, 1, 0, 0, None, None) == 0
-    assert lib.stairs_attend_workspace_bytes(None, 4, 1, 1) == 0
+    assert lib.stairs_attend_workspace_bytes(None, 4, 1, 1, 0) == 0
 
 
 @pytest.mark.parametrize("bad, code, text", [
