@@ -42,7 +42,7 @@ def build(force: bool = False, verbose: bool = False) -> str:
     """Compiles csrc/*.cu into libstairs_b200.so (skipped when up to date).  Returns the path."""
     if not force and not _stale():
         return LIB_PATH
-    jobs = [("engine.cu", []), ("attend.cu", []), ("attend_tc.cu", []), ("sample.cu", []), ("paged.cu", [])] + [("attend_mma.cu", ["-DATT_KS=%d" % ks]) for ks in ATTEND_STEPS] + [("forward.cu", ["-DFWD_HD=%d" % hd, "-DFWD_FAM=%d" % fam, "-DFWD_ATT=%d" % att, "-DFWD_ONE=%d" % one, "-DFWD_SHARE=%d" % share])
+    jobs = [("engine.cu", []), ("attend.cu", []), ("attend_tc.cu", []), ("attend_f32.cu", []), ("sample.cu", []), ("paged.cu", [])] + [("attend_mma.cu", ["-DATT_KS=%d" % ks]) for ks in ATTEND_STEPS] + [("forward.cu", ["-DFWD_HD=%d" % hd, "-DFWD_FAM=%d" % fam, "-DFWD_ATT=%d" % att, "-DFWD_ONE=%d" % one, "-DFWD_SHARE=%d" % share])
                                   for hd, fam, att, one, share in FORWARD]
     log = ""
     failed = False

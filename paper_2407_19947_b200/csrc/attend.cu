@@ -149,8 +149,9 @@ extern "C" int stairs_attend_static(const stairs_paged* cache, const int32_t* bl
   cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
   const Form f = form_of(cache, n_heads, n_req, n_rows, P.max_len);
   const int v = 16 / dtype_bytes(cache->dtype);
-  if (f.vectors && cache->dtype != DT_F32 && aligned16(q_dev) && q_row_stride % v == 0 && q_head_stride % v == 0 && aligned16(o_dev) && o_row_stride % v == 0 &&
+  if (f.vectors && aligned16(q_dev) && q_row_stride % v == 0 && q_head_stride % v == 0 && aligned16(o_dev) && o_row_stride % v == 0 &&
       o_head_stride % v == 0) {
+    if (cache->dtype == DT_F32) return launch_f32(P, st);
     const bool tc = f.tc && scale > 0.f;
     P.cluster = tc ? 0 : f.cluster;
     const size_t need = tc ? tc_workspace(cache->head_dim) : f.cluster ? 0 : am_workspace(f.ks, f.mg, cache->head_dim);

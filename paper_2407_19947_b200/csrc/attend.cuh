@@ -72,5 +72,8 @@ bool tc_takes(const stairs_paged* c, float scale);
 size_t tc_workspace(int hd);
 int launch_tc(const AttendParams& P, int dtype, cudaStream_t st);
 
+// --- 32-bit caches (attend_f32.cu) ------------------------------------------------------------------------------
+int launch_f32(AttendParams P, cudaStream_t st);
+
 }  // namespace att
 }  // namespace stairs

@@ -1,0 +1,293 @@
+// Attention over a caller's paged cache in 32 bits: fp32 caches, plain fused multiply-adds.
+//
+// The tensor cores hold no 32-bit mantissa, so both products run on the 128 multiply-adds a cycle of an SM: 4 queries x 4 positions (and 4 queries x HD / 16
+// columns) a thread, operands from shared memory as vectors, so that a multiply-add needs a quarter of a load.  A unit is (64 or 16 queries of a
+// request that share a key head, key head); K and V come in chunks of 64 positions with 16-byte asynchronous copies, K of the next chunk during
+// the softmax and the second product, V during the first.  Units of few queries leave most of a tile idle and are bound by the latency of their chunks;
+// the chunks of a unit are therefore cut over a cluster of CTAs where there are few units.
+#include <type_traits>
+
+#include "attend.cuh"
+
+namespace stairs {
+namespace att {
+namespace {
+
+constexpr int AF_CH = 64, AF_THREADS = 256;
+
+__device__ __forceinline__ void cp16(void* dst, const void* src, bool on) {   // zeros where off
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(smem_addr(dst)), "l"(src), "r"(on ? 16 : 0));
+}
+__device__ __forceinline__ void cp_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N> __device__ __forceinline__ void cp_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
+
+template <int HD, int QI> struct GeoF {       // QI: queries a thread
+  static constexpr int Q = 16 * QI;
+  static constexpr int PITCH = HD + 4;        // floats of a row of Q, K and V: rows 16 bytes apart in the banks
+  static constexpr int PP = AF_CH + 4;        // of a row of weights
+  static constexpr int SMEM = ((Q + 2 * AF_CH) * PITCH + Q * PP + 4 * Q) * 4 + 2 * AF_CH * 8;
+};
+
+// Thread (ty, tx) of 16 x 16: queries ty + 16 i, positions tx + 16 j of the scores; columns 4 tx + 64 k .. of the values.
+template <int HD, int QI>
+__global__ void __launch_bounds__(AF_THREADS, HD * QI <= 256 ? 2 : 1) k_attend_f32(const __grid_constant__ AttendParams P) {
+  typedef GeoF<HD, QI> G;
+  constexpr int AF_Q = G::Q;
+  constexpr int COLS = HD / 64;               // vectors of four columns a thread
+  extern __shared__ __align__(16) float af_sm[];
+  float* qs = af_sm;
+  float* ks = qs + AF_Q * G::PITCH;
+  float* vs = ks + AF_CH * G::PITCH;
+  float* ps = vs + AF_CH * G::PITCH;
+  float* row_m = ps + AF_Q * G::PP;           // state of this CTA's part, for its cluster: maxima, sums
+  float* row_l = row_m + AF_Q;
+  long long* place = reinterpret_cast<long long*>(row_l + 3 * AF_Q);   // [2][64] where the chunk's positions lie
+  const int tid = threadIdx.x, tx = tid & 15, ty = tid >> 4, group = P.heads / P.kv_heads;
+  const int S = P.cluster, rank = blockIdx.x % S;
+  wait_prerequisites();
+  // the unit's request: 32 requests at a time, every warp by itself
+  int unit = blockIdx.x / S, req = -1, blocks = 0;
+  Span sp{0, 0, 0};
+  for (int r0 = 0; r0 < P.n_req && req < 0; r0 += 32) {
+    const int lane = tid & 31;
+    Span s{0, 0, 0};
+    if (r0 + lane < P.n_req) s = request_span(P, r0 + lane);
+    const int v = (int)(((long long)s.n * group + AF_Q - 1) / AF_Q) * P.kv_heads;
+    int incl = v;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) { const int x = __shfl_up_sync(0xffffffffu, incl, o); if (lane >= o) incl += x; }
+    const unsigned here = __ballot_sync(0xffffffffu, unit >= incl - v && unit < incl);
+    if (here) {
+      const int src = __ffs(here) - 1;
+      req = r0 + src;
+      sp.first = __shfl_sync(0xffffffffu, s.first, src); sp.n = __shfl_sync(0xffffffffu, s.n, src); sp.len = __shfl_sync(0xffffffffu, s.len, src);
+      blocks = __shfl_sync(0xffffffffu, v, src);
+      unit -= __shfl_sync(0xffffffffu, incl - v, src);
+    } else unit -= __shfl_sync(0xffffffffu, incl, 31);
+  }
+  if (req < 0) return;                        // (all CTAs of the cluster)
+  // the latest block of queries first: it is the longest
+  const int qb = blocks / P.kv_heads - 1 - unit / P.kv_heads, h = unit % P.kv_heads, q0 = qb * AF_Q, rows = min(AF_Q, sp.n * group - q0);
+  const int seen = sp.len - sp.n + (q0 + rows - 1) / group + 1;   // positions that the last query sees
+  const int all = seen <= 0 ? 0 : (seen + AF_CH - 1) / AF_CH, c0 = (int)((long long)all * rank / S), c1 = (int)((long long)all * (rank + 1) / S);
+  const int* table = P.table + (size_t)req * P.max_blocks;
+  const float* kb = reinterpret_cast<const float*>(P.kc) + h * P.head_stride;
+  const float* vb = reinterpret_cast<const float*>(P.vc) + h * P.head_stride;
+  constexpr int PC = HD / 4;                  // 16-byte pieces of a row
+  const int pieces = P.hd / 4;
+  auto page_of = [&](int c) {                 // of this thread's position of chunk c (asked for a chunk ahead of its use)
+    const int p = c * AF_CH + tid;
+    return tid < AF_CH && c < c1 && p < sp.len ? table[p / P.page_tokens] : -1;
+  };
+  auto file = [&](int c, int page) {          // where chunk c's positions lie
+    if (tid < AF_CH) place[(c & 1) * AF_CH + tid] = page >= 0 && page < P.n_pages ? page * P.page_stride + ((c * AF_CH + tid) % P.page_tokens) * P.token_stride : -1;
+  };
+  auto copy = [&](float* dst, const float* base, int c) {
+    if (c < c1) {
+#pragma unroll
+      for (int i = 0; i < AF_CH * PC / AF_THREADS; ++i) {
+        const int it = i * AF_THREADS + tid, r = it / PC, x = it % PC;
+        const long long at = place[(c & 1) * AF_CH + r];
+        const bool on = at >= 0 && x < pieces;
+        cp16(dst + r * G::PITCH + 4 * x, base + (on ? at + 4 * x : 0), on);
+      }
+    }
+    cp_commit();
+  };
+  for (int it = tid; it < AF_Q * PC; it += AF_THREADS) {
+    const int r = it / PC, x = it % PC, qi = q0 + r, j = qi / group;
+    const bool on = r < rows && x < pieces;
+    cp16(qs + r * G::PITCH + 4 * x, reinterpret_cast<const float*>(P.q) + (on ? (sp.first + j) * P.q_row + (h * group + qi - j * group) * P.q_head + 4 * x : 0), on);
+  }
+  file(c0, page_of(c0));
+  int page = page_of(c0 + 1);
+  __syncthreads();
+  copy(ks, kb, c0);
+  copy(vs, vb, c0);
+  int last[QI];                               // last position that each of this thread's queries sees
+#pragma unroll
+  for (int i = 0; i < QI; ++i) { const int r = ty + 16 * i; last[i] = r < rows ? sp.len - sp.n + (q0 + r) / group : -1; }
+  const int first_last = sp.len - sp.n + q0 / group;
+  float m[QI], l[QI], o[QI][COLS][4];
+#pragma unroll
+  for (int i = 0; i < QI; ++i) {
+    m[i] = -INFINITY; l[i] = 0.f;
+#pragma unroll
+    for (int k = 0; k < COLS; ++k)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) o[i][k][e] = 0.f;
+  }
+  const float sc = P.scale;
+  for (int c = c0; c < c1; ++c) {
+    cp_wait<1>();                             // K (and the queries)
+    file(c + 1, page);
+    page = page_of(c + 2);
+    __syncthreads();
+    float s[QI][4];
+#pragma unroll
+    for (int i = 0; i < QI; ++i)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) s[i][j] = 0.f;
+#pragma unroll 4
+    for (int d = 0; d < HD; d += 4) {
+      float4 a[QI], b[4];
+#pragma unroll
+      for (int i = 0; i < QI; ++i) a[i] = *reinterpret_cast<const float4*>(qs + (ty + 16 * i) * G::PITCH + d);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) b[j] = *reinterpret_cast<const float4*>(ks + (tx + 16 * j) * G::PITCH + d);
+#pragma unroll
+      for (int i = 0; i < QI; ++i)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) s[i][j] = fmaf(a[i].w, b[j].w, fmaf(a[i].z, b[j].z, fmaf(a[i].y, b[j].y, fmaf(a[i].x, b[j].x, s[i][j]))));
+    }
+    const long long* at = place + (c & 1) * AF_CH;
+    const bool edge = c * AF_CH + AF_CH - 1 > first_last;
+#pragma unroll
+    for (int i = 0; i < QI; ++i) {
+      float mx = -INFINITY;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const int p = c * AF_CH + tx + 16 * j;
+        s[i][j] = p > last[i] || at[tx + 16 * j] < 0 ? -INFINITY : s[i][j] * sc;
+        mx = fmaxf(mx, s[i][j]);
+      }
+#pragma unroll
+      for (int w = 8; w > 0; w >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, w));
+      const float n = fmaxf(m[i], mx), ref = n == -INFINITY ? 0.f : n, f = expf(m[i] - ref);
+      float sum = 0.f;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) { s[i][j] = expf(s[i][j] - ref); sum += s[i][j]; ps[(ty + 16 * i) * G::PP + tx + 16 * j] = s[i][j]; }
+#pragma unroll
+      for (int w = 8; w > 0; w >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, w);
+      l[i] = l[i] * f + sum;
+      m[i] = n;
+      if (f != 1.f)
+#pragma unroll
+        for (int k = 0; k < COLS; ++k)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) o[i][k][e] *= f;
+    }
+    cp_wait<0>();                             // V
+    __syncthreads();                          // (and the weights; K has been read)
+    copy(ks, kb, c + 1);
+    // Positions hidden from some rows have weight zero there; infinities and NaN among their values are passed over one by one
+    auto add = [&](auto skip) {
+#pragma unroll 2
+      for (int p = 0; p < AF_CH; p += 4) {
+        float4 w[QI];
+#pragma unroll
+        for (int i = 0; i < QI; ++i) w[i] = *reinterpret_cast<const float4*>(ps + (ty + 16 * i) * G::PP + p);
+#pragma unroll
+        for (int z = 0; z < 4; ++z) {
+#pragma unroll
+          for (int k = 0; k < COLS; ++k) {
+            const float4 v = *reinterpret_cast<const float4*>(vs + (p + z) * G::PITCH + 4 * tx + 64 * k);
+#pragma unroll
+            for (int i = 0; i < QI; ++i) {
+              const float x = z == 0 ? w[i].x : z == 1 ? w[i].y : z == 2 ? w[i].z : w[i].w;
+              if (skip.value && c * AF_CH + p + z > last[i]) continue;
+              o[i][k][0] = fmaf(x, v.x, o[i][k][0]); o[i][k][1] = fmaf(x, v.y, o[i][k][1]); o[i][k][2] = fmaf(x, v.z, o[i][k][2]); o[i][k][3] = fmaf(x, v.w, o[i][k][3]);
+            }
+          }
+        }
+      }
+    };
+    if (edge) add(std::true_type{}); else add(std::false_type{});
+    __syncthreads();                          // V and the weights have been read
+    copy(vs, vb, c + 1);
+  }
+  cp_wait<0>();
+  auto store = [&](int r, int col, const float* v, float inv) {
+    const int qi = q0 + r, j = qi / group;
+    if (r < rows && col < P.hd)
+      *reinterpret_cast<float4*>(reinterpret_cast<float*>(P.o) + (sp.first + j) * P.o_row + (h * group + qi - j * group) * P.o_head + col) =
+          make_float4(v[0] * inv, v[1] * inv, v[2] * inv, v[3] * inv);
+  };
+  if (S == 1) {
+#pragma unroll
+    for (int i = 0; i < QI; ++i)
+#pragma unroll
+      for (int k = 0; k < COLS; ++k) store(ty + 16 * i, 4 * tx + 64 * k, o[i][k], m[i] == -INFINITY ? 0.f : 1.f / l[i]);
+    return;
+  }
+  // the parts' states, joined in the order of the positions; every CTA takes a share of the rows
+  float* xo = ks;                             // [64][HD + 4], K's place
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < QI; ++i) {
+    const int r = ty + 16 * i;
+    if (tx == 0) { row_m[r] = m[i]; row_l[r] = l[i]; }
+#pragma unroll
+    for (int k = 0; k < COLS; ++k) *reinterpret_cast<float4*>(xo + r * G::PITCH + 4 * tx + 64 * k) = make_float4(o[i][k][0], o[i][k][1], o[i][k][2], o[i][k][3]);
+  }
+  asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+  for (int it = rank * AF_THREADS + tid; it < rows * pieces; it += S * AF_THREADS) {
+    const int r = it / pieces, col = it % pieces * 4;
+    const uint32_t am = smem_addr(row_m + r), al = smem_addr(row_l + r), ao = smem_addr(xo + r * G::PITCH + col);
+    float mp[8], M = -INFINITY, L = 0.f, v[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int p = 0; p < 8; ++p) {
+      mp[p] = -INFINITY;
+      if (p < S) {
+        uint32_t at;
+        asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"(am), "r"(p));
+        asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(mp[p]) : "r"(at));
+      }
+      M = fmaxf(M, mp[p]);
+    }
+#pragma unroll
+    for (int p = 0; p < 8; ++p) {
+      if (mp[p] == -INFINITY) continue;
+      uint32_t at_l, at_o;
+      float lp, x[4];
+      asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at_l) : "r"(al), "r"(p));
+      asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at_o) : "r"(ao), "r"(p));
+      asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(lp) : "r"(at_l));
+      asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(x[0]), "=f"(x[1]), "=f"(x[2]), "=f"(x[3]) : "r"(at_o));
+      const float w = expf(mp[p] - M);
+      if (w == 0.f) continue;
+      L = fmaf(lp, w, L);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) v[e] = fmaf(x[e], w, v[e]);
+    }
+    store(r, col, v, M == -INFINITY ? 0.f : 1.f / L);
+  }
+  __syncwarp();
+  asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");   // (a CTA's shared memory is there until all have read it)
+}
+
+template <int HD, int QI> int launch(AttendParams& P, cudaStream_t st) {
+  typedef GeoF<HD, QI> G;
+  constexpr int AF_Q = G::Q;
+  auto kern = k_attend_f32<HD, QI>;
+  static_assert(G::SMEM <= 227 * 1024, "shared memory");
+  static std::atomic<unsigned long long> done{0};
+  if (int rc = allow_shared(done, reinterpret_cast<const void*>(kern), G::SMEM)) return rc;
+  const long long q = (long long)P.n_rows * (P.heads / P.kv_heads), blocks = P.n_req == 1 ? (q + AF_Q - 1) / AF_Q : q / AF_Q + P.n_req, units = blocks * P.kv_heads;
+  // CTAs a unit: as many as fill the SMs, and have a chunk each
+  const int chunks = (P.max_len + AF_CH - 1) / AF_CH, room = 128 * (HD * QI <= 256 ? 2 : 1);
+  P.cluster = 1;
+  while (P.cluster < 8 && units * P.cluster * 2 <= room && P.cluster < chunks) P.cluster *= 2;
+  if (units * P.cluster > 0x7fffffffll) return static_fail(STAIRS_ENOSPC, "stairs_attend_static: %d rows of %d heads are too many", P.n_rows, P.heads);
+  cudaLaunchConfig_t cfg{};
+  cfg.gridDim = dim3((unsigned)(units * P.cluster)); cfg.blockDim = dim3(AF_THREADS); cfg.dynamicSmemBytes = G::SMEM; cfg.stream = st;
+  cudaLaunchAttribute at[1];
+  at[0].id = cudaLaunchAttributeClusterDimension;
+  at[0].val.clusterDim.x = P.cluster; at[0].val.clusterDim.y = 1; at[0].val.clusterDim.z = 1;
+  cfg.attrs = at; cfg.numAttrs = P.cluster > 1 ? 1 : 0;
+  SCK(cudaLaunchKernelEx(&cfg, kern, P));
+  return STAIRS_OK;
+}
+
+}  // namespace
+
+int launch_f32(AttendParams P, cudaStream_t st) {
+  // 16 queries a unit where the average request has no more: 16 requests of 1000 tokens, one new one each, 32 heads of 80: 585 us in units of 64
+  const bool few = (long long)P.n_rows * (P.heads / P.kv_heads) <= 16ll * P.n_req;
+  if (P.hd <= 64) return few ? launch<64, 1>(P, st) : launch<64, 4>(P, st);
+  if (P.hd <= 128) return few ? launch<128, 1>(P, st) : launch<128, 4>(P, st);
+  return few ? launch<256, 1>(P, st) : launch<256, 4>(P, st);
+}
+
+}  // namespace att
+}  // namespace stairs
