@@ -377,6 +377,27 @@ int stairs_sample_static(const void *logits_dev, int dtype, int vocab, int64_t l
                          const int32_t *draft_dev, int k_max, int32_t *target_tokens_dev,
                          int32_t *accept_len_dev, void *stream);
 
+/* stairs_validate with a token drawn for every row as stairs_sample_static draws it, in place of the
+ * greedy one: target_tokens_dev, accept_len_dev and the tokens that commit != 0 appends are the drawn
+ * ones.  params_host [n_req]; u_dev [total_rows], rows ordered request by request; logits_dev fp32
+ * [total_rows, vocab] is required (scores of every row, out).  target_tokens_dev and accept_len_dev are
+ * device memory.  A row without a finite score draws -1, which commit appends as it is.
+ * Errors: those of stairs_validate and stairs_sample_static; a refused call has enqueued nothing. */
+int stairs_validate_sampled(stairs_ctx *ctx, int n_req, const int32_t *req_ids_host,
+                            const int32_t *k_host, const stairs_sampling *params_host,
+                            const float *u_dev, const int32_t *draft_dev, int32_t *target_tokens_dev,
+                            int32_t *accept_len_dev, float *logits_dev, int commit);
+
+/* stairs_generate with drawn tokens.  New token i is drawn with u_dev[i] (device, max_new numbers),
+ * whichever iteration and row it comes from, so the output depends on the prompt, the settings and u alone:
+ * it is the same for every k, and the one that a token-by-token loop draws (as far as the kernels give a
+ * row the same scores in passes of other row counts: bit for bit up to 64 rows of bf16 models, to rounding
+ * elsewhere).  scratch_dev: device memory for (k + 1) * vocab + 128 floats.  Waits for completion. */
+int stairs_generate_sampled(stairs_ctx *ctx, int req, const int32_t *prompt_host, int n_prompt,
+                            int k, int max_new, int32_t eos, const stairs_sampling *params_host,
+                            const float *u_dev, float *scratch_dev, int32_t *out_host,
+                            int32_t *n_out, stairs_stats *stats_or_null);
+
 #ifdef __cplusplus
 }
 #endif

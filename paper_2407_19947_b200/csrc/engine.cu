@@ -1950,6 +1950,33 @@ int stairs_validate(stairs_ctx* ctx, int n_req, const int32_t* req_ids_host, con
   return STAIRS_OK;
 }
 
+int stairs_validate_sampled(stairs_ctx* ctx, int n_req, const int32_t* req_ids_host, const int32_t* k_host, const stairs_sampling* params_host,
+                            const float* u_dev, const int32_t* draft_dev, int32_t* target_tokens_dev, int32_t* accept_len_dev, float* logits_dev, int commit) {
+  if (!ctx) return STAIRS_EINVAL;
+  if (n_req <= 0 || n_req > ctx->cfg.max_requests || !req_ids_host) return fail(ctx, STAIRS_EINVAL, "bad validate arguments");
+  const int vocab = ctx->cfg.target.vocab, k_max = ctx->cfg.k_max;
+  int rc = check_sample("stairs_validate_sampled", logits_dev, DT_F32, vocab, vocab, n_req, k_host, params_host, u_dev, draft_dev, k_max, target_tokens_dev, accept_len_dev);
+  if (rc) return fail(ctx, rc, "%s", stairs_last_error(nullptr));
+  // the scores (and the greedy walk, overwritten below), then the drawn tokens and their walk
+  if ((rc = stairs_validate(ctx, n_req, req_ids_host, k_host, draft_dev, target_tokens_dev, accept_len_dev, logits_dev, 0))) return rc;
+  rc = stairs_sample_static(logits_dev, DT_F32, vocab, vocab, n_req, k_host, params_host, u_dev, draft_dev, k_max, target_tokens_dev, accept_len_dev, ctx->stream);
+  if (rc) return fail(ctx, rc, "%s", stairs_last_error(nullptr));
+  ctx->launches += 2;
+  if (!commit) return STAIRS_OK;
+  for (int i0 = 0; i0 < n_req; i0 += COMMIT_REQ) {
+    CommitParams p{};
+    p.n_req = std::min(COMMIT_REQ, n_req - i0); p.k_max = k_max; p.max_seq_len = ctx->cfg.max_seq_len;
+    for (int i = 0; i < p.n_req; ++i) p.slot[i] = req_ids_host[i0 + i];
+    p.draft = draft_dev ? draft_dev + (size_t)i0 * k_max : nullptr; p.tokens = target_tokens_dev + (size_t)i0 * (k_max + 1); p.accept = accept_len_dev + i0;
+    p.seq = reinterpret_cast<int*>(ctx->ws + ctx->lay.seq); p.n_seq = reinterpret_cast<int*>(ctx->ws + ctx->lay.n_seq);
+    k_commit<<<(p.n_req + 63) / 64, 64, 0, ctx->stream>>>(p);
+    ctx->launches++;
+    CK(cudaGetLastError());
+  }
+  for (int i = 0; i < n_req; ++i) ctx->n_seq_ub[req_ids_host[i]] += k_host[i] + 1;
+  return STAIRS_OK;
+}
+
 int stairs_validate_host(stairs_ctx* ctx, int n_req, const int32_t* req_ids_host, const int32_t* k_host,
                          const int32_t* draft_host, int32_t* target_tokens_host, int32_t* accept_len_host, int commit) {
   if (!ctx) return STAIRS_EINVAL;
@@ -1984,8 +2011,10 @@ namespace {
 // The generation loop behind stairs_generate and stairs_generate_adaptive.  adaptive: the draft
 // length follows the acceptance (all drafts kept: two more next time, otherwise one fewer, never
 // below one), the schedule of the sequential assisted generation the paper compares with.
+// `drawn`: tokens are drawn (stairs_generate_sampled).
+struct Drawn { const stairs_sampling* s; const float* u_dev; float* scratch_dev; };
 int generate_loop(stairs_ctx* ctx, int req, const int32_t* prompt_host, int n_prompt, int k, int max_new,
-                  int32_t eos, int32_t* out_host, int32_t* n_out, stairs_stats* stats, bool adaptive) {
+                  int32_t eos, int32_t* out_host, int32_t* n_out, stairs_stats* stats, bool adaptive, const Drawn* drawn = nullptr) {
   int rc = check_slot(ctx, req, false);
   if (rc) return rc;
   if (!out_host || !n_out || max_new < 0) return fail(ctx, STAIRS_EINVAL, "bad generate arguments");
@@ -2012,8 +2041,12 @@ int generate_loop(stairs_ctx* ctx, int req, const int32_t* prompt_host, int n_pr
   // with one small copy into the same block
   int* tt_dev = ctx->io_dev + ctx->io_tt;
   int* al_dev = ctx->io_dev + ctx->io_al;
-  const int* tt = ctx->io_host + ctx->io_tt;
-  const int* al_h = ctx->io_host + ctx->io_al;
+  int* tt = ctx->io_host + ctx->io_tt;
+  int* al_h = ctx->io_host + ctx->io_al;
+  if (drawn) {   // (the walk over drawn tokens reads them again: they stay on the device and are copied back)
+    tt_dev = reinterpret_cast<int*>(drawn->scratch_dev + (size_t)(k + 1) * ctx->cfg.target.vocab);
+    al_dev = tt_dev + km + 1;
+  }
   int* draft_h = ctx->io_host + ctx->io_draft;
   (void)km;
   int produced = 0;
@@ -2025,9 +2058,13 @@ int generate_loop(stairs_ctx* ctx, int req, const int32_t* prompt_host, int n_pr
     if ((ce = cudaEventRecord(e1, ctx->stream)) != cudaSuccess) break;
     if (k_eff > 0 && (rc = stairs_draft(ctx, req, k_eff, d_dev))) break;
     if ((ce = cudaEventRecord(e2, ctx->stream)) != cudaSuccess) break;
-    if ((rc = stairs_validate(ctx, 1, &req, &k_eff, d_dev, tt_dev, al_dev, nullptr, 1))) break;
+    if (drawn) rc = stairs_validate_sampled(ctx, 1, &req, &k_eff, drawn->s, drawn->u_dev + produced, d_dev, tt_dev, al_dev, drawn->scratch_dev, 1);
+    else rc = stairs_validate(ctx, 1, &req, &k_eff, d_dev, tt_dev, al_dev, nullptr, 1);
+    if (rc) break;
     if ((ce = cudaEventRecord(e3, ctx->stream)) != cudaSuccess) break;
     if (k_eff > 0 && (ce = cudaMemcpyAsync(draft_h, d_dev, (size_t)k_eff * 4, cudaMemcpyDeviceToHost, ctx->stream)) != cudaSuccess) break;
+    if (drawn && ((ce = cudaMemcpyAsync(tt, tt_dev, (size_t)(k_eff + 1) * 4, cudaMemcpyDeviceToHost, ctx->stream)) != cudaSuccess ||
+                  (ce = cudaMemcpyAsync(al_h, al_dev, 4, cudaMemcpyDeviceToHost, ctx->stream)) != cudaSuccess)) break;
     if ((rc = stairs_sync(ctx))) break;
     const int al = al_h[0];
     ctx->n_seq_ub[req] += al - k_eff;
@@ -2071,6 +2108,19 @@ int stairs_generate_adaptive(stairs_ctx* ctx, int req, const int32_t* prompt_hos
                              int32_t eos, int32_t* out_host, int32_t* n_out, stairs_stats* stats) {
   if (ctx && k_first < 1) return fail(ctx, STAIRS_EINVAL, "k_first=%d: the adaptive schedule starts from at least one drafted token", k_first);
   return generate_loop(ctx, req, prompt_host, n_prompt, k_first, max_new, eos, out_host, n_out, stats, true);
+}
+
+int stairs_generate_sampled(stairs_ctx* ctx, int req, const int32_t* prompt_host, int n_prompt, int k, int max_new, int32_t eos,
+                            const stairs_sampling* params_host, const float* u_dev, float* scratch_dev, int32_t* out_host, int32_t* n_out,
+                            stairs_stats* stats_or_null) {
+  if (!ctx) return STAIRS_EINVAL;
+  if (k < 0 || k > ctx->cfg.k_max) return fail(ctx, STAIRS_EINVAL, "k=%d outside 0..k_max", k);
+  const int32_t none = 0, vocab = ctx->cfg.target.vocab;
+  // (the settings and buffers are checked before the prompt is run; the addresses that stand for the results are not followed)
+  const int rc = check_sample("stairs_generate_sampled", scratch_dev, DT_F32, vocab, vocab, 1, &none, params_host, u_dev, nullptr, ctx->cfg.k_max, &none, &none);
+  if (rc) return fail(ctx, rc, "%s", stairs_last_error(nullptr));
+  const Drawn d{params_host, u_dev, scratch_dev};
+  return generate_loop(ctx, req, prompt_host, n_prompt, k, max_new, eos, out_host, n_out, stats_or_null, false, &d);
 }
 
 int stairs_sequence(stairs_ctx* ctx, int req, int32_t* seq_host, int capacity, int32_t* n_seq) {

@@ -299,6 +299,25 @@ static __global__ void k_accept(AcceptParams p) {
   }
 }
 
+// The commit step of k_accept by itself, for tokens that were drawn: the kept drafts, then the token drawn behind the last kept one.
+constexpr int COMMIT_REQ = 256;
+struct CommitParams {
+  int n_req, k_max, max_seq_len;
+  int slot[COMMIT_REQ];
+  const int* draft; const int* tokens; const int* accept;
+  int* seq; int* n_seq;
+};
+static __global__ void k_commit(const __grid_constant__ CommitParams p) {
+  const int i = blockIdx.x * blockDim.x + threadIdx.x;
+  if (i >= p.n_req) return;
+  const int slot = p.slot[i], a = p.accept[i];
+  int* s = p.seq + (size_t)slot * p.max_seq_len;
+  int w = p.n_seq[slot];
+  for (int r = 0; r < a && w < p.max_seq_len; ++r) s[w++] = p.draft[i * p.k_max + r];
+  if (w < p.max_seq_len) s[w++] = p.tokens[i * (p.k_max + 1) + a];
+  p.n_seq[slot] = w;
+}
+
 // Assistant step epilogue: the argmax of one row becomes drafted token j.
 static __global__ void k_take_token(const unsigned long long* __restrict__ keys, int row, int* __restrict__ out, int j) {
   if (threadIdx.x == 0 && blockIdx.x == 0) out[j] = argmax_key_index(keys[row]);

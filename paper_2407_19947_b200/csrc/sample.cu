@@ -749,19 +749,16 @@ template <typename T> int launch_sample(SampleParams& P, cudaStream_t st) {
 
 using namespace stairs;
 
-extern "C" int stairs_sample_static(const void* logits_dev, int dtype, int vocab, int64_t ld, int n_req, const int32_t* k_host,
-                                    const stairs_sampling* params_host, const float* u_dev, const int32_t* draft_dev, int k_max,
-                                    int32_t* target_tokens_dev, int32_t* accept_len_dev, void* stream) {
-  const char* who = "stairs_sample_static";
+int stairs::check_sample(const char* who, const void* logits_dev, int dtype, int vocab, long long ld, int n_req, const int32_t* k_host, const stairs_sampling* params_host,
+                         const float* u_dev, const int32_t* draft_dev, int k_max, const int32_t* target_tokens_dev, const int32_t* accept_len_dev) {
   if (!logits_dev || !k_host || !params_host || !u_dev || !target_tokens_dev || !accept_len_dev) return static_fail(STAIRS_EINVAL, "%s: NULL buffer", who);
   if (dtype < DT_F32 || dtype > DT_F16) return static_fail(STAIRS_EINVAL, "%s: dtype %d", who, dtype);
-  if (vocab < 1 || ld < vocab) return static_fail(STAIRS_EINVAL, "%s: vocab=%d, ld=%lld", who, vocab, (long long)ld);
+  if (vocab < 1 || ld < vocab) return static_fail(STAIRS_EINVAL, "%s: vocab=%d, ld=%lld", who, vocab, ld);
   if (vocab > (1 << 20)) return static_fail(STAIRS_EUNSUPPORTED, "%s: vocab=%d above 2^20", who, vocab);
   if (reinterpret_cast<uintptr_t>(logits_dev) % dtype_bytes(dtype)) return static_fail(STAIRS_EINVAL, "%s: logits_dev is not aligned to its type", who);
   if (n_req < 1 || n_req > STAIRS_SAMPLE_MAX_REQ) return static_fail(STAIRS_ENOSPC, "%s: n_req=%d outside 1..%d", who, n_req, STAIRS_SAMPLE_MAX_REQ);
   if (k_max < 0 || k_max > 63) return static_fail(STAIRS_EINVAL, "%s: k_max=%d outside 0..63", who, k_max);
-  SampleParams P{};
-  int rows = 0, top = 0;
+  int rows = 0;
   for (int i = 0; i < n_req; ++i) {
     const stairs_sampling& s = params_host[i];
     if (k_host[i] < 0 || k_host[i] > k_max) return static_fail(STAIRS_EINVAL, "%s: k[%d]=%d outside 0..k_max=%d", who, i, k_host[i], k_max);
@@ -771,11 +768,24 @@ extern "C" int stairs_sample_static(const void* logits_dev, int dtype, int vocab
     if (s.top_k < 0) return static_fail(STAIRS_EINVAL, "%s: top_k[%d]=%d is negative", who, i, s.top_k);
     if (!(s.top_p > 0.f && s.top_p <= 1.f)) return static_fail(STAIRS_EINVAL, "%s: top_p[%d]=%g outside (0, 1]", who, i, s.top_p);
     if (!(s.min_p >= 0.f && s.min_p <= 1.f)) return static_fail(STAIRS_EINVAL, "%s: min_p[%d]=%g outside [0, 1]", who, i, s.min_p);
-    P.s[i] = s; P.k[i] = k_host[i]; P.off[i] = rows;
+    rows += k_host[i] + 1;
+  }
+  if (rows > STAIRS_STATIC_MAX_ROWS) return static_fail(STAIRS_ENOSPC, "%s: %d rows above %d", who, rows, STAIRS_STATIC_MAX_ROWS);
+  return STAIRS_OK;
+}
+
+extern "C" int stairs_sample_static(const void* logits_dev, int dtype, int vocab, int64_t ld, int n_req, const int32_t* k_host,
+                                    const stairs_sampling* params_host, const float* u_dev, const int32_t* draft_dev, int k_max,
+                                    int32_t* target_tokens_dev, int32_t* accept_len_dev, void* stream) {
+  if (int rc = check_sample("stairs_sample_static", logits_dev, dtype, vocab, ld, n_req, k_host, params_host, u_dev, draft_dev, k_max, target_tokens_dev, accept_len_dev))
+    return rc;
+  SampleParams P{};
+  int rows = 0, top = 0;
+  for (int i = 0; i < n_req; ++i) {
+    P.s[i] = params_host[i]; P.k[i] = k_host[i]; P.off[i] = rows;
     rows += k_host[i] + 1;
     top = std::max(top, k_host[i]);
   }
-  if (rows > STAIRS_STATIC_MAX_ROWS) return static_fail(STAIRS_ENOSPC, "%s: %d rows above %d", who, rows, STAIRS_STATIC_MAX_ROWS);
   P.logits = logits_dev; P.u = u_dev; P.draft = draft_dev; P.tokens = target_tokens_dev; P.accept = accept_len_dev;
   P.ld = ld; P.vocab = vocab; P.n_req = n_req; P.n_rows = rows; P.k_max = k_max;
   int lg = 0;

@@ -40,6 +40,10 @@ inline bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 
 // Checks that every entry point with a cache makes; 0 or a status with its text filed.
 int check_paged(const char* who, const stairs_paged* c);
 
+// The checks of stairs_sample_static on what the host can see, without launching anything; `who` goes into the text.
+int check_sample(const char* who, const void* logits_dev, int dtype, int vocab, long long ld, int n_req, const int32_t* k_host, const stairs_sampling* params_host,
+                 const float* u_dev, const int32_t* draft_dev, int k_max, const int32_t* target_tokens_dev, const int32_t* accept_len_dev);
+
 // PDL: the next kernel of the stream may be set up; wait until the previous one's writes are visible.
 __device__ __forceinline__ void launch_dependents() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
 __device__ __forceinline__ void wait_prerequisites() { asm volatile("griddepcontrol.wait;" ::: "memory"); }

@@ -24,7 +24,8 @@ EXPORTS = ["stairs_workspace_bytes", "stairs_init", "stairs_prefill", "stairs_dr
            "stairs_validate_host", "stairs_generate", "stairs_generate_adaptive", "stairs_sequence", "stairs_truncate", "stairs_sync",
            "stairs_launch_count", "stairs_profile", "stairs_profile_read", "stairs_reset",
            "stairs_destroy", "stairs_last_error", "stairs_accept_static", "stairs_tables_static",
-           "stairs_append_static", "stairs_attend_workspace_bytes", "stairs_attend_static", "stairs_sample_static", "stairs_debug_buffer", "stairs_debug_tune"]
+           "stairs_append_static", "stairs_attend_workspace_bytes", "stairs_attend_static", "stairs_sample_static",
+           "stairs_validate_sampled", "stairs_generate_sampled", "stairs_debug_buffer", "stairs_debug_tune"]
 
 STATIC_MAX_ROWS, STATIC_MAX_REQ = 1024, 64
 SAMPLE_MAX_REQ, TABLES_MAX_REQ, ATTEND_MAX_REQ, MAX_HEAD_DIM = 256, 4096, 4096, 256
@@ -118,6 +119,8 @@ def load_library(path: Optional[str] = None):
     lib.stairs_attend_static.argtypes = [vp, vp, C.c_int, C.c_int, vp, vp, C.c_int, C.c_int, C.c_int, vp, C.c_int64,
                                          C.c_int64, C.c_float, vp, C.c_int64, C.c_int64, vp, C.c_size_t, vp]
     lib.stairs_sample_static.argtypes = [vp, C.c_int, C.c_int, C.c_int64, C.c_int, i32p, vp, vp, vp, C.c_int, vp, vp, vp]
+    lib.stairs_validate_sampled.argtypes = [vp, C.c_int, i32p, i32p, vp, vp, vp, vp, vp, vp, C.c_int]
+    lib.stairs_generate_sampled.argtypes = [vp, C.c_int, i32p, C.c_int, C.c_int, C.c_int, C.c_int32, vp, vp, vp, i32p, i32p, C.POINTER(CStats)]
     lib.stairs_last_error.restype = C.c_char_p
     lib.stairs_last_error.argtypes = [vp]
     for name in EXPORTS:
@@ -299,6 +302,41 @@ class Stairs:
         self._ck(fn(self.h, req, _ptr(p), len(p), k, max_new, eos, _ptr(out), C.byref(n_out), C.byref(st)))
         stats = {n: getattr(st, n) for n, _ in CStats._fields_}
         return [int(x) for x in out[: n_out.value]], stats
+
+    def validate_sampled(self, req_ids: Sequence[int], k: Sequence[int], draft_dev, u, *, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0, commit=False):
+        """stairs_validate_sampled: (drawn tokens [n, k_max + 1], accept_len [n], logits [rows, vocab]), all on the device.  u: float32
+        random numbers in [0, 1), one a row; the settings are a number for all requests or one for each."""
+        t = self.torch
+        r, kk = _ints(req_ids), _ints(k)
+        n, rows = len(r), sum(kk[:]) + len(r)
+        _t()
+        if u.dtype != t.float32 or u.numel() < rows or not u.is_contiguous() or u.device != self._dev:
+            _refuse("u has to be one contiguous float32 number a row, on the context's device")
+        if draft_dev is not None and (draft_dev.dtype != t.int32 or draft_dev.numel() < n * self.k_max or not draft_dev.is_contiguous()):
+            _refuse("draft_dev has to be int32 [n_req, k_max]")
+        if len(kk) != n:
+            _refuse("k has to be one draft length for each request")
+        tt, al = t.zeros((n, self.k_max + 1), dtype=t.int32, device=self._dev), t.empty(n, dtype=t.int32, device=self._dev)
+        logits = t.empty((rows, self.vocab), dtype=t.float32, device=self._dev)
+        self._ck(self.lib.stairs_validate_sampled(self.h, n, r, kk, _settings(n, temperature, top_k, top_p, min_p), u.data_ptr(),
+                                                  draft_dev.data_ptr() if draft_dev is not None else None, tt.data_ptr(), al.data_ptr(),
+                                                  logits.data_ptr(), int(commit)))
+        return tt, al, logits
+
+    def generate_sampled(self, req: int, prompt: Sequence[int], k: int, max_new: int, u, *, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0, eos: int = -1):
+        """stairs_generate_sampled: (new_tokens list, stats dict).  u: float32 [max_new] random numbers on the device; new token i is drawn with
+        u[i], so the output is the same for every k."""
+        _t()
+        if u.dtype != self.torch.float32 or u.numel() < max_new or not u.is_contiguous() or u.device != self._dev:
+            _refuse("u has to be max_new contiguous float32 numbers on the context's device")
+        p = _i32(prompt)
+        out = np.zeros(max(max_new, 1), np.int32)
+        n_out = C.c_int32(0)
+        st = CStats()
+        scratch = self.torch.empty((max(k, 0) + 1) * self.vocab + 128, dtype=self.torch.float32, device=self._dev)
+        self._ck(self.lib.stairs_generate_sampled(self.h, req, _ptr(p), len(p), k, max_new, eos, _settings(1, temperature, top_k, top_p, min_p), u.data_ptr(),
+                                                  scratch.data_ptr(), _ptr(out), C.byref(n_out), C.byref(st)))
+        return [int(x) for x in out[: n_out.value]], {n: getattr(st, n) for n, _ in CStats._fields_}
 
     def sequence(self, req: int) -> List[int]:
         cap = self.cfg.max_seq_len
