@@ -178,7 +178,9 @@ __global__ void __launch_bounds__(AT_THREADS, 1) k_attend_tc(const __grid_consta
   uint8_t* vst = kst + NST * KBYTES;
   uint64_t* k_full = reinterpret_cast<uint64_t*>(vst + NST * KBYTES);
   uint64_t* k_empty = k_full + NST; uint64_t* v_full = k_empty + NST; uint64_t* v_empty = v_full + NST;
-  uint64_t* v_fixed = v_empty + NST;                // the stage's edge chunk has been cleaned
+  // Values of edge chunks arrive on barriers of their own: the warps that clean them wait for every phase of those, while a wait for one phase
+  // in many of v_full would be let through by an older phase of the same parity.
+  uint64_t* e_full = v_empty + NST; uint64_t* v_fixed = e_full + NST;   // v_fixed: the stage's edge chunk has been cleaned
   uint64_t* q_full = v_fixed + NST; uint64_t* q_empty = q_full + 1;
   uint64_t* s_full = q_empty + 1;                   // [2 tiles]
   uint64_t* p_full = s_full + 2; uint64_t* o_full = p_full + 2; uint64_t* o_free = o_full + 2;
@@ -199,7 +201,7 @@ __global__ void __launch_bounds__(AT_THREADS, 1) k_attend_tc(const __grid_consta
   launch_dependents();
   wait_prerequisites();
   if (tid == 0) {
-    for (int s = 0; s < NST; ++s) { mbar_init(k_full + s, 1); mbar_init(k_empty + s, 1); mbar_init(v_full + s, 1); mbar_init(v_empty + s, 1); mbar_init(v_fixed + s, 2); }
+    for (int s = 0; s < NST; ++s) { mbar_init(k_full + s, 1); mbar_init(k_empty + s, 1); mbar_init(v_full + s, 1); mbar_init(v_empty + s, 1); mbar_init(e_full + s, 1); mbar_init(v_fixed + s, 2); }
     mbar_init(q_full, 2); mbar_init(q_empty, 1); mbar_init(x_full, 4); mbar_init(x_free, 4);
     for (int t = 0; t < 2; ++t) { mbar_init(s_full + t, 1); mbar_init(p_full + t, 4); mbar_init(o_full + t, 1); mbar_init(o_free + t, 4); }
     *abort_flag = 0;
@@ -334,6 +336,7 @@ __global__ void __launch_bounds__(AT_THREADS, 1) k_attend_tc(const __grid_consta
       const Unit& u = W.u;
       if (seen_chunks(u)) {
         const int* table = P.table + (size_t)u.req * P.max_blocks;
+        const int edge = first_edge(u);
         auto page_of = [&](int c) {
           const int p = c * AT_CH + sl * J.box_rows;
           return half < HALVES && p < u.len ? __ldg(table + p / P.page_tokens) : -1;
@@ -346,7 +349,7 @@ __global__ void __launch_bounds__(AT_THREADS, 1) k_attend_tc(const __grid_consta
           const int token = (c * AT_CH + sl * J.box_rows) % P.page_tokens, pg = is ? page : P.n_pages;
           const int s = fills % NST, par = ((fills / NST) & 1) ^ 1;
           for (int v = 0; v < 2 && ok; ++v) {
-            uint64_t* full = (v ? v_full : k_full) + s;
+            uint64_t* full = (v ? c >= edge ? e_full : v_full : k_full) + s;
             ok = __all_sync(0xffffffffu, mbar_wait((v ? v_empty : k_empty) + s, par, abort_flag, AT_WAIT));
             if (!ok) break;
             if (lane == 0) { if (v == 0) valid_ring[fills % AT_RING] = valid; mbar_expect_tx(full, KBYTES); }
@@ -366,7 +369,7 @@ __global__ void __launch_bounds__(AT_THREADS, 1) k_attend_tc(const __grid_consta
     if (lane == 0) {
       const uint32_t idesc_s = instr_desc<BF>(AT_CH, 0), idesc_o = instr_desc<BF>(HD, 1);
       const uint64_t q_desc = desc_sw128(smem_u32(qs), 16, 1024), k_desc = desc_sw128(smem_u32(kst), 16, 1024), v_desc = desc_sw128(smem_u32(vst), AT_CH * 128, 1024);
-      int it = 0, fix[NST] = {}, pc[2] = {0, 0}, oc[2] = {0, 0};
+      int it = 0, fix[NST] = {}, plain[NST] = {}, pc[2] = {0, 0}, oc[2] = {0, 0};
       bool ok = true;
       auto scores = [&](int t, int qt, int i) {      // S of tile t (queries of tile qt) with the chunk in stage i % NST
         const uint64_t qd = q_desc + (uint64_t)(qt * (QTILE >> 4)), kd = k_desc + (uint64_t)((i % NST) * (KBYTES >> 4));   // (addresses in units of 16 bytes)
@@ -394,10 +397,7 @@ __global__ void __launch_bounds__(AT_THREADS, 1) k_attend_tc(const __grid_consta
         const int L = sh.L, edge = first_edge(u) - c0;   // (chunks from `edge` on are cleaned first)
         auto v_wait = [&](int j) {
           const int vs = (it + j) % NST;
-          if (j < edge) return mbar_wait(v_full + vs, ((it + j) / NST) & 1, abort_flag, AT_WAIT);
-          const bool r = mbar_wait(v_fixed + vs, fix[vs] & 1, abort_flag, AT_WAIT);
-          ++fix[vs];
-          return r;
+          return j < edge ? mbar_wait(v_full + vs, plain[vs]++ & 1, abort_flag, AT_WAIT) : mbar_wait(v_fixed + vs, fix[vs]++ & 1, abort_flag, AT_WAIT);
         };
         ok = mbar_wait(q_full, W.seg & 1, abort_flag, AT_WAIT);
         if (ok && L) {
@@ -441,7 +441,7 @@ __global__ void __launch_bounds__(AT_THREADS, 1) k_attend_tc(const __grid_consta
   } else if (warp >= 10) {
     // ------------------------------------------------------------------ queries, and values of chunks at the edge
     const int ft = tid - 320, pieces = P.hd / 8;
-    int it = 0;
+    int it = 0, edges[NST] = {};
     bool ok = true;
     while (ok && W.begin(c0, c1)) {
       const Unit& u = W.u;
@@ -467,7 +467,8 @@ __global__ void __launch_bounds__(AT_THREADS, 1) k_attend_tc(const __grid_consta
       __syncwarp();
       for (int j = max(edge, 0); j < L && ok; ++j) {
         const int s = (it + j) % NST;
-        ok = __all_sync(0xffffffffu, mbar_wait(v_full + s, ((it + j) / NST) & 1, abort_flag, AT_WAIT));
+        ok = __all_sync(0xffffffffu, mbar_wait(e_full + s, edges[s] & 1, abort_flag, AT_WAIT));
+        ++edges[s];
         if (!ok) break;
         constexpr uint32_t EXPO = BF ? 0x7f80u : 0x7c00u;
         const int left = u.len - (c0 + j) * AT_CH;   // positions of the chunk that the request has
@@ -801,11 +802,7 @@ __global__ void __launch_bounds__(AT_THREADS, 1) k_attend_tc(const __grid_consta
   if (*abort_flag) {
     if (warp == 8 && lane == 0) {
       const long long t0 = clock64();
-      for (int f = max(0, fills - NST); f <= fills; ++f)      // (the last one may have been requested for K alone)
-        for (int v = 0; v < 2; ++v)
-          while (!mbar_try((v ? v_full : k_full) + f % NST, (f / NST) & 1))
-            if (clock64() - t0 > 2000000) break;
-      settle(t0);
+      settle(t0);                                   // (copies in flight land within a millisecond, a thousand times what they take)
     }
     __syncthreads();
   }

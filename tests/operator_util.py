@@ -34,9 +34,9 @@ def tables_ref(n_seq, n_new, n_blocks, table, free, n_used, page, max_rows):
     return dict(out, table=table, n_used=[used], n_served=[served])
 
 
-def attend_ref(q, k_cache, v_cache, table, row_off, kv_len, scale, max_len=None):
+def attend_ref(q, k_cache, v_cache, table, row_off, kv_len, scale, max_len=None, rows_of=None):
     """(o in 64 bits, the bound of its error by the score's and the weights' roundings) - row by row, only of what a row sees.
-    Rows of no request are NaN in o."""
+    Rows of no request, and those that rows_of (a choice of rows) leaves out, are NaN in o."""
     pages, page, hkv, hd = k_cache.shape
     rows, heads, _ = q.shape
     group = heads // hkv
@@ -48,6 +48,8 @@ def attend_ref(q, k_cache, v_cache, table, row_off, kv_len, scale, max_len=None)
         a, b = int(row_off[r]), int(row_off[r + 1])
         length = max(0, length if max_len is None else min(length, max_len))
         for t in range(a, min(b, rows)):
+            if rows_of is not None and not rows_of(t):
+                continue
             last = length - (b - a) + (t - a)
             p = torch.arange(max(last + 1, 0), device=q.device)
             at = table[r][p // page].long()

@@ -146,7 +146,7 @@ class Paged:
         self.g = g
 
 
-def check_attend(st, p, q, new, lens, scale=None, slack=0, max_len=0, out=None):
+def check_attend(st, p, q, new, lens, scale=None, slack=0, max_len=0, out=None, rows_of=None):
     rows = sum(new)
     off, kv = i32(np.concatenate([[0], np.cumsum(new)]).tolist()), i32(lens)
     mark = 7.25
@@ -157,7 +157,7 @@ def check_attend(st, p, q, new, lens, scale=None, slack=0, max_len=0, out=None):
     got = st.attend_static(padded if slack else q, p.k, p.v, p.table, off, kv, scale=scale, out=out, max_len=max_len)
     assert got is out
     torch.cuda.synchronize()
-    want, tol = ou.attend_ref(q, p.k, p.v, p.table, off, kv, s, max_len or None)
+    want, tol = ou.attend_ref(q, p.k, p.v, p.table, off, kv, s, max_len or None, rows_of)
     asked = ~torch.isnan(want[:rows])
     assert bool((out[rows:] == mark).all()), "rows of no request were written"
     err = (out[:rows].double() - want[:rows]).abs()
@@ -195,6 +195,17 @@ def test_attend_long_and_wide(st, dtype, heads, hkv, hd, new, length):
     p = Paged(new + length, DTYPES[dtype], hkv, hd, 64, [length])
     q = (torch.randn((new, heads, hd), generator=p.g, device=DEV) * 1.5).to(DTYPES[dtype])
     check_attend(st, p, q, [new], [length])
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+@pytest.mark.parametrize("heads,hkv,hd,n,new,length", [(16, 8, 128, 6, 20, 5000), (32, 8, 128, 4, 9, 9000), (12, 12, 64, 12, 40, 3000), (8, 4, 80, 20, 33, 2500),
+                                                       (8, 8, 128, 3, 600, 2500), (16, 16, 64, 2, 700, 1500), (4, 4, 128, 40, 140, 900)])
+def test_attend_long_parts(st, dtype, heads, hkv, hd, n, new, length):
+    # a CTA's share is long: dozens of chunks before the ones that some row does not see, several units
+    lens = [length - (37 if n < 40 else 7) * r for r in range(n)]
+    p = Paged(n + new, DTYPES[dtype], hkv, hd, 64, lens)
+    q = (torch.randn((n * new, heads, hd), generator=p.g, device=DEV) * 1.5).to(DTYPES[dtype])
+    check_attend(st, p, q, [new] * n, lens, rows_of=lambda t: t % 7 == 0 or t % new >= new - 2)
 
 
 @pytest.mark.parametrize("dtype", ["fp32", "bf16"])
