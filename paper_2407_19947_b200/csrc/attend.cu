@@ -145,7 +145,9 @@ extern "C" int stairs_attend_static(const stairs_paged* cache, const int32_t* bl
   const int reach = max_blocks * cache->page_tokens;
   AttendParams P{cache->k_dev, cache->v_dev, q_dev, o_dev, cache->page_stride, cache->token_stride, cache->head_stride, q_row_stride, q_head_stride,
                  o_row_stride, o_head_stride, block_table_dev, row_off_dev, kv_len_dev, n_req, n_rows, n_heads, cache->n_kv_heads, cache->head_dim,
-                 cache->n_pages, cache->page_tokens, max_blocks, max_len ? std::min(max_len, reach) : reach, scale, workspace, 0};
+                 cache->n_pages, cache->page_tokens, max_blocks, max_len ? std::min(max_len, reach) : reach, scale, workspace, -1, 0};
+  if ((cache->page_tokens & (cache->page_tokens - 1)) == 0)
+    for (P.page_shift = 0; (1 << P.page_shift) < cache->page_tokens;) ++P.page_shift;
   cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
   const Form f = form_of(cache, n_heads, n_req, n_rows, P.max_len);
   const int v = 16 / dtype_bytes(cache->dtype);

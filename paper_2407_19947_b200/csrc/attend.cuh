@@ -12,6 +12,7 @@ struct AttendParams {
   int n_req, n_rows, heads, kv_heads, hd, n_pages, page_tokens, max_blocks, max_len;
   float scale;
   void* ws;                     // caller's scratch
+  int page_shift;               // log2 of page_tokens, or -1
   int cluster;                  // split form: CTAs that share a unit; 0: units cut evenly over all CTAs
 };
 

@@ -169,9 +169,11 @@ __global__ void __launch_bounds__(MG * 128 + 64, am_ctas(KS, MG)) k_attend_mma(c
     if (S) { unit = (int)rem0; chunk = chunk0; }
     else { unit = (int)divide(rem0, chunks); chunk = (int)(rem0 - (long long)unit * chunks); }
     int seg = 0, part_begin = chunk, planned = 0;
-    Step plan;                                  // the step being planned, and this thread's position's place
-    long long place = -1;
-    auto plan_load = [&]() {                    // step `planned` (its table entry is on the way when this returns)
+    // A step is planned in two halves, a step apart: its place in the list, with the table entry of this thread's position asked for, and, when that
+    // has arrived, where the position lies.
+    Step plan;
+    int page = -1, at_token = 0, filed = 0;
+    auto plan_load = [&]() {
       if (planned >= n_steps) return;
       plan.first = sp.first; plan.n = sp.n; plan.len = sp.len;
       plan.qb = unit / P.kv_heads; plan.h = unit - plan.qb * P.kv_heads; plan.chunk = chunk;
@@ -180,10 +182,11 @@ __global__ void __launch_bounds__(MG * 128 + 64, am_ctas(KS, MG)) k_attend_mma(c
       plan.ends = (unit_ends || last) && !S ? ((part_begin > 0 || !unit_ends) ? 2 : 1) : 0;
       plan.slot = 2 * blockIdx.x + (seg ? 1 : 0);
       const int p = chunk * AM_CHUNK + ct;
-      place = -1;
+      page = -1;
       if (p < sp.len) {
-        const int b = p / P.page_tokens, page = __ldg(P.table + (size_t)req * P.max_blocks + b);
-        if (page >= 0 && page < P.n_pages) place = page * P.page_stride + (p - b * P.page_tokens) * P.token_stride;
+        const int b = P.page_shift >= 0 ? p >> P.page_shift : p / P.page_tokens;
+        at_token = p - b * P.page_tokens;
+        page = __ldg(P.table + (size_t)req * P.max_blocks + b);
       }
       if (plan.ends == 2) { const long long u0 = x0 + planned - chunk; plan.cut = cut_of(u0, u0 + chunks, total, parts_all); }
       if (unit_ends) {
@@ -194,10 +197,12 @@ __global__ void __launch_bounds__(MG * 128 + 64, am_ctas(KS, MG)) k_attend_mma(c
           units = units_of(sp);
         }
       } else ++chunk;
+      ++planned;
     };
     auto plan_store = [&]() {
-      if (planned < n_steps) {
-        const int slot = planned % G::R;
+      if (filed < planned) {
+        const int slot = filed % G::R;
+        const long long place = page >= 0 && page < P.n_pages ? page * P.page_stride + at_token * P.token_stride : -1;
         roff[slot * AM_CHUNK + ct] = place;
         const unsigned v = __ballot_sync(0xffffffffu, place >= 0);
         Step* s = steps + slot;
@@ -206,7 +211,7 @@ __global__ void __launch_bounds__(MG * 128 + 64, am_ctas(KS, MG)) k_attend_mma(c
           s->first = plan.first; s->n = plan.n; s->len = plan.len; s->qb = plan.qb; s->h = plan.h; s->chunk = plan.chunk;
           s->begins = plan.begins; s->ends = plan.ends; s->slot = plan.slot; s->cut = plan.cut;
         }
-        ++planned;
+        ++filed;
       }
     };
     const int pieces = P.hd / 8;                // 16-byte pieces of a head that exist
@@ -247,20 +252,21 @@ __global__ void __launch_bounds__(MG * 128 + 64, am_ctas(KS, MG)) k_attend_mma(c
       cp_commit();
     };
     auto copiers_sync = []() { asm volatile("bar.sync 2, 64;" ::: "memory"); };
-    for (int i = 0; i < NST - 1; ++i) {         // (copies of a step are on their way before the next one is planned)
-      plan_load();
+    plan_load();
+    for (int i = 0; i < NST - 1; ++i) {         // (copies of a step are on their way before the next one's place is needed)
       plan_store();
+      plan_load();
       copiers_sync();
       issue(i);
     }
-    plan_load();
     plan_store();
+    plan_load();
     for (int x = 0; x < n_steps; ++x) {
       cp_wait<NST - 2>();
       __syncthreads();                          // step x has arrived; its predecessor's stage and entry are free
       issue(x + NST - 1);
+      plan_store();                             // (step x + NST)
       plan_load();
-      plan_store();
     }
     cp_wait<0>();
     if (S > 1) { cluster_sync(); cluster_sync(); }
