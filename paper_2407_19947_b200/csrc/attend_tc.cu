@@ -199,7 +199,6 @@ __global__ void __launch_bounds__(AT_THREADS, 1) k_attend_tc(const __grid_consta
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int group = P.heads / P.kv_heads;
   launch_dependents();
-  wait_prerequisites();
   if (tid == 0) {
     for (int s = 0; s < NST; ++s) { mbar_init(k_full + s, 1); mbar_init(k_empty + s, 1); mbar_init(v_full + s, 1); mbar_init(v_empty + s, 1); mbar_init(e_full + s, 1); mbar_init(v_fixed + s, 2); }
     mbar_init(q_full, 2); mbar_init(q_empty, 1); mbar_init(x_full, 4); mbar_init(x_free, 4);
@@ -870,10 +869,11 @@ int launch_tc(const AttendParams& P, int dtype, cudaStream_t st) {
   }
   TcParams J;
   J.a = P;
-  // units of 128 queries where the average request has no more, and where units of 256 would be few: each would be cut into many parts, which its
-  // last warp reads one by one (one request, 256 queries a key head after 16384 tokens: wide 169 us)
+  // units of 128 queries where the average request has no more, and where units of 256 would be very few: each would be cut into many parts, which
+  // its last warp reads one by one (8 key heads of 128; 132 queries a key head after 16384 tokens: one request, 8 units of 256, 74 us narrow and 160
+  // wide; four requests, 32 units, 143 and 129; sixteen after 1000 tokens 88 and 81)
   const long long q = (long long)P.n_rows * (P.heads / P.kv_heads), wide_units = (q + 255) / 256 * P.kv_heads;
-  const bool narrow = q <= 128ll * P.n_req || wide_units < AM_SMS / 2;
+  const bool narrow = q <= 128ll * P.n_req || wide_units < 16;
   const int ch = narrow ? Form<true>::CH : Form<false>::CH;
   J.box_rows = P.page_tokens < ch ? P.page_tokens : ch;
   // the coordinates between the elements and the pages: the one of the smaller stride first
