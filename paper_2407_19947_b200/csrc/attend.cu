@@ -20,7 +20,6 @@ using namespace att;
 constexpr int AP_WARPS = 4;
 template <typename T> __global__ void __launch_bounds__(AP_WARPS * 32) k_attend_plain(const AttendParams P) {
   __shared__ float qs[STAIRS_MAX_HEAD_DIM], accs[AP_WARPS][STAIRS_MAX_HEAD_DIM], ms[AP_WARPS], ls[AP_WARPS];
-  wait_prerequisites();
   const int h = blockIdx.x % P.heads, t = blockIdx.x / P.heads, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   int lo = 0, hi = P.n_req - 1;              // the last request whose first row is <= t
   while (lo < hi) {
@@ -141,8 +140,10 @@ extern "C" int stairs_attend_static(const stairs_paged* cache, const int32_t* bl
   if (!(fabsf(scale) < INFINITY)) return static_fail(STAIRS_EINVAL, "%s: scale is not finite", who);
   if (n_rows == 0) return STAIRS_OK;
   if (!q_dev || !o_dev) return static_fail(STAIRS_EINVAL, "%s: NULL buffer", who);
+  if (!aligned(q_dev, dtype_bytes(cache->dtype)) || !aligned(o_dev, dtype_bytes(cache->dtype)) || !aligned(block_table_dev, 4) || !aligned(row_off_dev, 4) || !aligned(kv_len_dev, 4))
+    return static_fail(STAIRS_EINVAL, "%s: a buffer is not aligned to its type", who);
   if ((long long)n_rows * n_heads > 0x7fffffffll) return static_fail(STAIRS_ENOSPC, "%s: %d rows of %d heads are too many", who, n_rows, n_heads);
-  const int reach = max_blocks * cache->page_tokens;
+  const int reach = std::min(max_blocks * cache->page_tokens, 0x7fffffff - 1024);   // (positions of a chunk that passes it stay within 31 bits)
   AttendParams P{cache->k_dev, cache->v_dev, q_dev, o_dev, cache->page_stride, cache->token_stride, cache->head_stride, q_row_stride, q_head_stride,
                  o_row_stride, o_head_stride, block_table_dev, row_off_dev, kv_len_dev, n_req, n_rows, n_heads, cache->n_kv_heads, cache->head_dim,
                  cache->n_pages, cache->page_tokens, max_blocks, max_len ? std::min(max_len, reach) : reach, scale, workspace, -1, 0};

@@ -44,7 +44,6 @@ __global__ void __launch_bounds__(AF_THREADS, HD * QI <= 256 ? 2 : 1) k_attend_f
   long long* place = reinterpret_cast<long long*>(row_l + 3 * AF_Q);   // [2][64] where the chunk's positions lie
   const int tid = threadIdx.x, tx = tid & 15, ty = tid >> 4, group = P.heads / P.kv_heads;
   const int S = P.cluster, rank = blockIdx.x % S;
-  wait_prerequisites();
   // the unit's request: 32 requests at a time, every warp by itself
   int unit = blockIdx.x / S, req = -1, blocks = 0;
   Span sp{0, 0, 0};

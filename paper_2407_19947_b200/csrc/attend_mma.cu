@@ -73,7 +73,6 @@ __global__ void __launch_bounds__(MG * 128 + 64, am_ctas(KS, MG)) k_attend_mma(c
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, pw = warp & 3, mg = warp >> 2;
   const int group = P.heads / P.kv_heads;
   launch_dependents();
-  wait_prerequisites();
 
   // this CTA's part of the list
   const int S = P.cluster, rank = S ? blockIdx.x % S : 0;

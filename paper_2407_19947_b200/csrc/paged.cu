@@ -10,6 +10,7 @@ namespace stairs {
 int check_paged(const char* who, const stairs_paged* c) {
   if (!c || !c->k_dev || !c->v_dev) return static_fail(STAIRS_EINVAL, "%s: NULL cache", who);
   if (c->dtype < DT_F32 || c->dtype > DT_F16) return static_fail(STAIRS_EINVAL, "%s: cache dtype %d", who, c->dtype);
+  if (!aligned(c->k_dev, dtype_bytes(c->dtype)) || !aligned(c->v_dev, dtype_bytes(c->dtype))) return static_fail(STAIRS_EINVAL, "%s: the cache is not aligned to its type", who);
   if (c->n_pages < 1 || c->page_tokens < 1 || c->n_kv_heads < 1 || c->head_dim < 1)
     return static_fail(STAIRS_EINVAL, "%s: cache of %d pages, %d tokens a page, %d heads of %d", who, c->n_pages, c->page_tokens, c->n_kv_heads, c->head_dim);
   if (c->head_dim > STAIRS_MAX_HEAD_DIM) return static_fail(STAIRS_EUNSUPPORTED, "%s: head_dim %d above %d", who, c->head_dim, STAIRS_MAX_HEAD_DIM);
@@ -52,7 +53,6 @@ __global__ void __launch_bounds__(TB_THREADS) k_tables(const TablesParams P) {
   __shared__ long long w_pages[TB_THREADS / 32], w_rows[TB_THREADS / 32];
   __shared__ int s_served;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  wait_prerequisites();
   const int used0 = P.n_used_in[0];
   if (tid == 0) { s_served = P.n_req; s_off[0] = 0; }
   long long pages_before = 0, rows_before = 0;
@@ -140,7 +140,6 @@ struct AppendParams {
 // elements of the call fit (64-bit divisions took 2048 rows of 32 x 80 from 7 to 12 us).
 template <typename S, typename D, int VEC, typename INDEX>
 __global__ void __launch_bounds__(256) k_append(const AppendParams P) {
-  wait_prerequisites();
   const INDEX pieces = P.head_dim / VEC, per_row = P.heads * pieces, it = (INDEX)blockIdx.x * 256 + threadIdx.x;
   if (it >= (INDEX)P.n_rows * per_row) return;
   const INDEX t = it / per_row, in_row = it - t * per_row, h = in_row / pieces, i = (in_row - h * pieces) * VEC;
@@ -189,6 +188,11 @@ extern "C" int stairs_tables_static(int n_req, const int32_t* n_seq_dev, const i
   if (!n_seq_dev || !n_new_dev || !n_blocks_in_dev || !block_table_dev || !n_used_in_dev || !n_blocks_out_dev || !n_used_out_dev || !row_off_dev ||
       !kv_len_dev || !n_served_dev || (n_free > 0 && !free_dev) || (max_rows > 0 && (!row_req_dev || !row_pos_dev || !row_slot_dev)))
     return static_fail(STAIRS_EINVAL, "%s: NULL buffer", who);
+  for (const void* p : {(const void*)n_seq_dev, (const void*)n_new_dev, (const void*)n_blocks_in_dev, (const void*)block_table_dev, (const void*)free_dev, (const void*)n_used_in_dev,
+                        (const void*)n_blocks_out_dev, (const void*)n_used_out_dev, (const void*)row_off_dev, (const void*)kv_len_dev, (const void*)row_req_dev,
+                        (const void*)row_pos_dev, (const void*)n_served_dev})
+    if (!aligned(p, 4)) return static_fail(STAIRS_EINVAL, "%s: a buffer is not aligned to its numbers", who);
+  if (!aligned(row_slot_dev, 8)) return static_fail(STAIRS_EINVAL, "%s: a buffer is not aligned to its numbers", who);
   if (n_req < 1 || n_req > STAIRS_TABLES_MAX_REQ) return static_fail(STAIRS_ENOSPC, "%s: n_req=%d outside 1..%d", who, n_req, STAIRS_TABLES_MAX_REQ);
   if (max_blocks < 1 || page_tokens < 1 || n_free < 0 || max_rows < 0)
     return static_fail(STAIRS_EINVAL, "%s: max_blocks=%d, page_tokens=%d, n_free=%d, max_rows=%d", who, max_blocks, page_tokens, n_free, max_rows);
@@ -216,6 +220,8 @@ extern "C" int stairs_append_static(const stairs_paged* cache, int n_rows, const
   if (dtype < DT_F32 || dtype > DT_F16) return static_fail(STAIRS_EINVAL, "%s: dtype %d", who, dtype);
   if (n_rows == 0) return STAIRS_OK;
   if (!k_new_dev || !v_new_dev || !row_slot_dev) return static_fail(STAIRS_EINVAL, "%s: NULL buffer", who);
+  if (!aligned(k_new_dev, dtype_bytes(dtype)) || !aligned(v_new_dev, dtype_bytes(dtype)) || !aligned(row_slot_dev, 8))
+    return static_fail(STAIRS_EINVAL, "%s: a buffer is not aligned to its type", who);
   AppendParams P{k_new_dev, v_new_dev, cache->k_dev, cache->v_dev, reinterpret_cast<const long long*>(row_slot_dev), row_stride, head_stride,
                  cache->page_stride, cache->token_stride, cache->head_stride, (long long)cache->n_pages * cache->page_tokens,
                  n_rows, cache->n_kv_heads, cache->head_dim, cache->page_tokens};

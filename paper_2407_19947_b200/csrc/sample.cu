@@ -139,7 +139,6 @@ __global__ void __launch_bounds__(SP_THREADS, 2) k_sample(const __grid_constant_
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, row = blockIdx.x / CL, rank = blockIdx.x % CL, V = P.vocab;
   launch_dependents();
   if (CL > 1) asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");
-  wait_prerequisites();
   int lo_r = 0, hi_r = P.n_req - 1;
   while (lo_r < hi_r) {
     const int mid = (lo_r + hi_r + 1) >> 1;
@@ -756,6 +755,8 @@ int stairs::check_sample(const char* who, const void* logits_dev, int dtype, int
   if (vocab < 1 || ld < vocab) return static_fail(STAIRS_EINVAL, "%s: vocab=%d, ld=%lld", who, vocab, ld);
   if (vocab > (1 << 20)) return static_fail(STAIRS_EUNSUPPORTED, "%s: vocab=%d above 2^20", who, vocab);
   if (reinterpret_cast<uintptr_t>(logits_dev) % dtype_bytes(dtype)) return static_fail(STAIRS_EINVAL, "%s: logits_dev is not aligned to its type", who);
+  if (!aligned(u_dev, 4) || !aligned(draft_dev, 4) || !aligned(target_tokens_dev, 4) || !aligned(accept_len_dev, 4))
+    return static_fail(STAIRS_EINVAL, "%s: a buffer is not aligned to its numbers", who);
   if (n_req < 1 || n_req > STAIRS_SAMPLE_MAX_REQ) return static_fail(STAIRS_ENOSPC, "%s: n_req=%d outside 1..%d", who, n_req, STAIRS_SAMPLE_MAX_REQ);
   if (k_max < 0 || k_max > 63) return static_fail(STAIRS_EINVAL, "%s: k_max=%d outside 0..63", who, k_max);
   int rows = 0;

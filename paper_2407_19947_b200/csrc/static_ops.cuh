@@ -35,7 +35,8 @@ inline int allow_shared(std::atomic<unsigned long long>& done, const void* kern,
 enum Dtype { DT_F32 = 0, DT_BF16 = 1, DT_F16 = 2 };
 inline int dtype_bytes(int dt) { return dt == DT_F32 ? 4 : 2; }
 
-inline bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
+inline bool aligned(const void* p, int bytes) { return reinterpret_cast<uintptr_t>(p) % (size_t)bytes == 0; }
+inline bool aligned16(const void* p) { return aligned(p, 16); }
 
 // Checks that every entry point with a cache makes; 0 or a status with its text filed.
 int check_paged(const char* who, const stairs_paged* c);

@@ -166,7 +166,7 @@ def check_attend(st, p, q, new, lens, scale=None, slack=0, max_len=0, out=None, 
     return out
 
 
-SHAPES = [(4, 4, 64), (32, 8, 128), (8, 8, 80), (8, 1, 128), (6, 2, 16), (12, 4, 40), (4, 2, 96), (3, 3, 8), (2, 1, 256), (5, 5, 24), (4, 2, 192), (16, 1, 32), (64, 1, 64)]
+SHAPES = [(4, 4, 64), (32, 8, 128), (8, 8, 80), (8, 1, 128), (6, 2, 16), (12, 4, 40), (4, 2, 96), (3, 3, 8), (2, 1, 256), (5, 5, 24), (4, 2, 192), (16, 1, 32), (64, 1, 64), (3, 1, 20), (2, 2, 7), (6, 3, 1)]
 
 
 @pytest.mark.parametrize("dtype", ["fp32", "bf16", "fp16"])
@@ -217,6 +217,19 @@ def test_attend_many_requests_of_every_length(st, dtype):
     p = Paged(3, DTYPES[dtype], 2, 64, 16, lens, "HND")
     q = torch.randn((sum(new), 4, 64), generator=p.g, device=DEV).to(DTYPES[dtype])
     check_attend(st, p, q, new, lens)
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16", "fp16"])
+@pytest.mark.parametrize("n,hd,new", [(100, 64, 1), (40, 128, 3), (200, 32, 2)])
+def test_attend_many_short_requests_of_one_key_head(st, dtype, n, hd, new):
+    rng = np.random.default_rng(n)
+    lens = rng.integers(1, 200, n).tolist()
+    rows = [int(min(a, rng.integers(0, new + 1))) for a in lens]
+    p = Paged(n, DTYPES[dtype], 1, hd, 32, lens)
+    q = torch.randn((sum(rows), 4, hd), generator=p.g, device=DEV).to(DTYPES[dtype])
+    check_attend(st, p, q, rows, lens, max_len=max(lens))
+    check_attend(st, p, q, rows, lens, max_len=1 << 20, scale=-0.2)
+    check_attend(st, p, q, rows, lens, scale=0.0)
 
 
 @pytest.mark.parametrize("dtype", ["fp32", "bf16", "fp16"])
@@ -442,6 +455,18 @@ def test_sample_many_rows(st, dtype):
         u = torch.rand(rows, generator=g, device=DEV)
         drafts = x.float().argmax(1).view(n, k + 1)[:, : max(k, 1)].int().contiguous()
         check_sample(st, x, [k] * n, u, [SETTINGS[i % len(SETTINGS)] for i in range(n)], drafts)
+
+
+@pytest.mark.parametrize("dtype,vocab", [("fp32", 1 << 20), ("bf16", 400001), ("fp32", 300000), ("bf16", 1 << 20)])
+def test_sample_large_vocabularies(st, dtype, vocab):
+    g = gen(vocab)
+    n = 6
+    x = torch.randn((n, vocab), generator=g, device=DEV) * 2
+    x[0] = 1.0
+    x[1, vocab - 1] = 30.0
+    x[2, : vocab - 5] = -math.inf
+    u = torch.rand(n, generator=g, device=DEV)
+    check_sample(st, x.to(DTYPES[dtype]), [0] * n, u, [(1.0, 0, 0.7, 0.0), (1.0, 0, 1.0, 0.0), (1.0, 3, 1.0, 0.0), (0.8, 600, 0.95, 0.0), (1.5, 0, 0.98, 0.0), (0.7, 40, 1.0, 0.1)])
 
 
 def test_sample_distribution(st):

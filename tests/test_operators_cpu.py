@@ -34,10 +34,11 @@ def said(lib, rc, want, text):
     (dict(table=None), EINVAL, "NULL"), (dict(free=None), EINVAL, "NULL"), (dict(slot=None), EINVAL, "NULL"), (dict(served=None), EINVAL, "NULL"),
     (dict(page=0), EINVAL, "page_tokens"), (dict(blocks=0), EINVAL, "max_blocks"), (dict(blocks=1 << 27, page=16), EINVAL, "31 bits"),
     (dict(n_free=-1), EINVAL, "n_free"), (dict(rows=-1), EINVAL, "max_rows"), (dict(rows=2**31 - 1), EINVAL, "max_rows"),
-    (dict(blocks_out=P + 1), EINVAL, "output is its input"), (dict(used_out=P + 2), EINVAL, "output is its input")])
+    (dict(blocks_out=P + 4), EINVAL, "output is its input"), (dict(used_out=P + 8), EINVAL, "output is its input"),
+    (dict(kv=P + 2), EINVAL, "aligned"), (dict(slot=P + 4), EINVAL, "aligned")])
 def test_tables_refusals(lib, bad, code, text):
-    a = dict(n_req=2, n_seq=P, n_new=P, blocks_in=P + 1, table=P, blocks=8, page=16, free=P, n_free=4, used_in=P + 2, rows=10, blocks_out=P + 3,
-             used_out=P + 4, off=P, kv=P, req=P, pos=P, slot=P, served=P)
+    a = dict(n_req=2, n_seq=P, n_new=P, blocks_in=P + 4, table=P, blocks=8, page=16, free=P, n_free=4, used_in=P + 8, rows=10, blocks_out=P + 12,
+             used_out=P + 16, off=P, kv=P, req=P, pos=P, slot=P, served=P)
     a.update(bad)
     said(lib, lib.stairs_tables_static(*a.values(), None), code, text)
 
@@ -45,7 +46,8 @@ def test_tables_refusals(lib, bad, code, text):
 @pytest.mark.parametrize("bad, code, text", [
     (dict(c=None), EINVAL, "NULL"), (dict(c=cache(k_dev=None)), EINVAL, "NULL"), (dict(c=cache(dtype=3)), EINVAL, "dtype"), (dict(c=cache(head_dim=0)), EINVAL, "heads of 0"),
     (dict(c=cache(head_dim=257)), EUNSUPPORTED, "head_dim"), (dict(c=cache(page_stride=-1)), EINVAL, "stride"), (dict(c=cache(n_pages=0)), EINVAL, "pages"),
-    (dict(rows=-1), EINVAL, "n_rows"), (dict(k=None), EINVAL, "NULL"), (dict(dtype=-1), EINVAL, "dtype"), (dict(row_stride=-2), EINVAL, "stride"), (dict(slot=None), EINVAL, "NULL")])
+    (dict(rows=-1), EINVAL, "n_rows"), (dict(k=None), EINVAL, "NULL"), (dict(dtype=-1), EINVAL, "dtype"), (dict(row_stride=-2), EINVAL, "stride"), (dict(slot=None), EINVAL, "NULL"),
+    (dict(k=P + 1), EINVAL, "aligned"), (dict(slot=P + 4), EINVAL, "aligned"), (dict(c=cache(v_dev=P + 1)), EINVAL, "aligned")])
 def test_append_refusals(lib, bad, code, text):
     a = dict(c=cache(), rows=3, k=P, v=P, dtype=1, row_stride=128, head_stride=64, slot=P)
     a.update(bad)
@@ -66,9 +68,21 @@ def attend(lib, **bad):
     (dict(n_req=0), ENOSPC, "n_req"), (dict(n_req=4097), ENOSPC, "n_req"), (dict(blocks=0), EINVAL, "max_blocks"), (dict(blocks=1 << 27), EINVAL, "max_blocks"),
     (dict(max_len=-1), EINVAL, "max_len"), (dict(rows=-1), EINVAL, "n_rows"), (dict(q_row=-1), EINVAL, "stride"), (dict(heads=3), EINVAL, "heads"),
     (dict(heads=0), EINVAL, "heads"), (dict(scale=float("nan")), EINVAL, "scale"), (dict(scale=float("inf")), EINVAL, "scale"), (dict(rows=1 << 30), ENOSPC, "rows"),
-    (dict(c=cache(head_dim=264)), EUNSUPPORTED, "head_dim")])
+    (dict(c=cache(head_dim=264)), EUNSUPPORTED, "head_dim"), (dict(q=P + 1), EINVAL, "aligned"), (dict(o=P + 1), EINVAL, "aligned"), (dict(kv=P + 2), EINVAL, "aligned"),
+    (dict(rows=4096, ws=None), EINVAL, "scratch"), (dict(rows=4096, ws=(1 << 20) + 64), EINVAL, "scratch"), (dict(rows=4096, ws_bytes=1000), ENOSPC, "scratch"),
+    (dict(n_req=300, ws=None), EINVAL, "scratch"), (dict(n_req=300, ws_bytes=1000), ENOSPC, "scratch")])
 def test_attend_refusals(lib, bad, code, text):
     said(lib, attend(lib, **bad), code, text)
+
+
+def test_attend_scratch_grows_with_what_is_unknown(lib):
+    c = cache(n_pages=64)
+    ask = lambda rows, n, length: lib.stairs_attend_workspace_bytes(C.byref(c), 4, n, rows, length)  # noqa: E731
+    assert ask(1, 1, 128) == 0                       # a small call needs none
+    assert ask(1, 1, 0) > 0 and ask(4096, 1, 128) > 0
+    assert ask(1, 1, -1) == 0 and ask(0, 1, 1) == 0 and lib.stairs_attend_workspace_bytes(C.byref(c), 3, 1, 1, 1) == 0
+    for rows in (1, 9, 40, 300):                     # what is enough for a bound is enough for a smaller one, 0 standing for any
+        assert ask(rows, 3, 0) >= ask(rows, 3, 100000) >= ask(rows, 3, 1000) >= ask(rows, 3, 10) >= 0
 
 
 def test_calls_of_no_rows_enqueue_nothing(lib):
@@ -80,7 +94,7 @@ def test_calls_of_no_rows_enqueue_nothing(lib):
 
 @pytest.mark.parametrize("bad, code, text", [
     (dict(logits=None), EINVAL, "NULL"), (dict(u=None), EINVAL, "NULL"), (dict(dtype=5), EINVAL, "dtype"), (dict(vocab=0), EINVAL, "vocab"), (dict(ld=99), EINVAL, "ld"),
-    (dict(vocab=(1 << 20) + 1, ld=1 << 21), EUNSUPPORTED, "2^20"), (dict(logits=P + 2, dtype=0), EINVAL, "aligned"), (dict(n=0), ENOSPC, "n_req"), (dict(n=257), ENOSPC, "n_req"),
+    (dict(vocab=(1 << 20) + 1, ld=1 << 21), EUNSUPPORTED, "2^20"), (dict(logits=P + 2, dtype=0), EINVAL, "aligned"), (dict(u=P + 2), EINVAL, "aligned"), (dict(n=0), ENOSPC, "n_req"), (dict(n=257), ENOSPC, "n_req"),
     (dict(k_max=64), EINVAL, "k_max"), (dict(k=5), EINVAL, "k[1]"), (dict(k=-1), EINVAL, "k[1]"), (dict(draft=None), EINVAL, "draft_dev"),
     (dict(t=-0.5), EINVAL, "temperature[1]"), (dict(t=float("nan")), EINVAL, "temperature[1]"), (dict(t=1e-7), EINVAL, "temperature[1]"), (dict(t=float("inf")), EINVAL, "temperature[1]"),
     (dict(top_k=-1), EINVAL, "top_k[1]"), (dict(top_p=0.0), EINVAL, "top_p[1]"), (dict(top_p=1.5), EINVAL, "top_p[1]"), (dict(top_p=float("nan")), EINVAL, "top_p[1]"),
