@@ -871,9 +871,9 @@ int launch_tc(const AttendParams& P, int dtype, cudaStream_t st) {
   J.a = P;
   // units of 128 queries where the average request has no more, and where units of 256 would be very few: each would be cut into many parts, which
   // its last warp reads one by one (8 key heads of 128; 132 queries a key head after 16384 tokens: one request, 8 units of 256, 74 us narrow and 160
-  // wide; four requests, 32 units, 143 and 129; sixteen after 1000 tokens 88 and 81)
+  // wide; two after 8192, 16 units, 66 and 97; four after 16384, 32 units, 143 and 129; sixteen after 1000 tokens 88 and 81)
   const long long q = (long long)P.n_rows * (P.heads / P.kv_heads), wide_units = (q + 255) / 256 * P.kv_heads;
-  const bool narrow = q <= 128ll * P.n_req || wide_units < 16;
+  const bool narrow = q <= 128ll * P.n_req || wide_units <= 16;
   const int ch = narrow ? Form<true>::CH : Form<false>::CH;
   J.box_rows = P.page_tokens < ch ? P.page_tokens : ch;
   // the coordinates between the elements and the pages: the one of the smaller stride first
