@@ -285,8 +285,8 @@ typedef struct stairs_paged {
  *                                n_seq + n_new tokens are entered behind those it holds
  *   free_dev, n_free             int32 list of free pages; entries n_used_in_dev[0].. are handed out
  *                                in order, first to request 0
- *   n_blocks_out_dev, n_used_out_dev (out) the two counts after the call; not the same memory as
- *                                the inputs
+ *   n_blocks_out_dev, n_used_out_dev (out) the two counts after the call.  No output may overlap
+ *                                an input or another output
  *   row_off_dev, kv_len_dev      (out) int32 [n_req + 1], [n_req]: first row of each request, and
  *                                its length with the new tokens
  *   row_req_dev, row_pos_dev     (out) int32 [max_rows]: request and position of every row
@@ -310,7 +310,8 @@ int stairs_tables_static(int n_req, const int32_t *n_seq_dev, const int32_t *n_n
  * t*row_stride + head*head_stride + i, type `dtype`) goes to slot row_slot_dev[t] of the cache,
  * rounded to the cache's type (to nearest, ties to even; beyond its range: infinity).  Rows whose
  * slot is no slot of the cache (negative, or n_pages * page_tokens and up) are skipped.  A slot named
- * twice gets one of the two rows, for keys and values each on its own.  n_rows may be 0. */
+ * twice gets one of the two rows, every 16 bytes on its own.  The rows may not overlap the cache.
+ * n_rows may be 0. */
 int stairs_append_static(const stairs_paged *cache, int n_rows, const void *k_new_dev,
                          const void *v_new_dev, int dtype, int64_t row_stride, int64_t head_stride,
                          const int64_t *row_slot_dev, void *stream);
@@ -364,8 +365,9 @@ typedef struct stairs_sampling {
  * row that has no other gets -1.  Where x holds +infinity, only such tokens weigh (1 each).
  * A drafted token is kept while it equals the token drawn for the row before it, so the
  * tokens kept and the one after them are distributed as the model's own, drawn one by one.
- * Weights are held to 2^-47 of the largest and summed exactly, so a row's token depends neither on
- * the rest of the call nor on the device's timing.
+ * Weights are held to 2^-b of the largest, b = min(47, 62 - ceil(log2 vocab)), and summed exactly, so
+ * a row's token depends neither on the rest of the call nor on the device's timing.  u outside [0, 1) is
+ * taken as the nearest number within, NaN as 0.
  *   logits_dev          [n_rows, ld] of `dtype`, rows request by request
  *   params_host         [n_req]
  *   draft_dev, k_max, target_tokens_dev, accept_len_dev   as for stairs_accept_static

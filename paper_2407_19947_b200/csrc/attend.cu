@@ -140,6 +140,7 @@ extern "C" int stairs_attend_static(const stairs_paged* cache, const int32_t* bl
   if (!(fabsf(scale) < INFINITY)) return static_fail(STAIRS_EINVAL, "%s: scale is not finite", who);
   if (n_rows == 0) return STAIRS_OK;
   if (!q_dev || !o_dev) return static_fail(STAIRS_EINVAL, "%s: NULL buffer", who);
+  if (q_dev == o_dev) return static_fail(STAIRS_EINVAL, "%s: the result lies over the queries", who);   // (parts of a row's positions read its queries at different times)
   if (!aligned(q_dev, dtype_bytes(cache->dtype)) || !aligned(o_dev, dtype_bytes(cache->dtype)) || !aligned(block_table_dev, 4) || !aligned(row_off_dev, 4) || !aligned(kv_len_dev, 4))
     return static_fail(STAIRS_EINVAL, "%s: a buffer is not aligned to its type", who);
   if ((long long)n_rows * n_heads > 0x7fffffffll) return static_fail(STAIRS_ENOSPC, "%s: %d rows of %d heads are too many", who, n_rows, n_heads);

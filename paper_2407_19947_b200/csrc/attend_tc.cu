@@ -859,13 +859,15 @@ bool tc_takes(const stairs_paged* c, float scale) {
 size_t tc_workspace(int hd) { return (size_t)AM_SMS * (64 + (size_t)2 * 256 * (hd + 2) * 4) + 256; }
 
 int launch_tc(const AttendParams& P, int dtype, cudaStream_t st) {
-  static EncodeFn encode = nullptr;              // (the driver's function: the same whoever looks it up)
+  static std::atomic<EncodeFn> looked_up{nullptr};   // (the driver's function: the same whoever looks it up)
+  EncodeFn encode = looked_up.load(std::memory_order_acquire);
   if (!encode) {
     void* fn = nullptr;
     cudaDriverEntryPointQueryResult q;
     SCK(cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &fn, cudaEnableDefault, &q));
     if (!fn || q != cudaDriverEntryPointSuccess) return static_fail(STAIRS_ECUDA, "cuTensorMapEncodeTiled is not available from the driver");
     encode = reinterpret_cast<EncodeFn>(fn);
+    looked_up.store(encode, std::memory_order_release);
   }
   TcParams J;
   J.a = P;

@@ -198,7 +198,9 @@ extern "C" int stairs_tables_static(int n_req, const int32_t* n_seq_dev, const i
     return static_fail(STAIRS_EINVAL, "%s: max_blocks=%d, page_tokens=%d, n_free=%d, max_rows=%d", who, max_blocks, page_tokens, n_free, max_rows);
   if ((long long)max_blocks * page_tokens >= (1ll << 31)) return static_fail(STAIRS_EINVAL, "%s: max_blocks * page_tokens beyond 31 bits", who);
   if (max_rows > 0x7fffffff - TB_ROWS) return static_fail(STAIRS_EINVAL, "%s: max_rows=%d", who, max_rows);
-  if (n_blocks_out_dev == n_blocks_in_dev || n_used_out_dev == n_used_in_dev) return static_fail(STAIRS_EINVAL, "%s: a count's output is its input", who);
+  for (const int32_t* out : {(const int32_t*)n_blocks_out_dev, (const int32_t*)n_used_out_dev, (const int32_t*)row_off_dev, (const int32_t*)kv_len_dev})
+    for (const int32_t* in : {n_seq_dev, n_new_dev, n_blocks_in_dev, n_used_in_dev})   // (one block would read what another has written)
+      if (out == in) return static_fail(STAIRS_EINVAL, "%s: an output is its input", who);
   TablesParams P{n_req, max_blocks, page_tokens, n_free, max_rows, n_seq_dev, n_new_dev, n_blocks_in_dev, free_dev, n_used_in_dev,
                  block_table_dev, n_blocks_out_dev, n_used_out_dev, row_off_dev, kv_len_dev, row_req_dev, row_pos_dev,
                  reinterpret_cast<long long*>(row_slot_dev), n_served_dev};

@@ -312,8 +312,9 @@ class Stairs:
         _t()
         if u.dtype != t.float32 or u.numel() < rows or not u.is_contiguous() or u.device != self._dev:
             _refuse("u has to be one contiguous float32 number a row, on the context's device")
-        if draft_dev is not None and (draft_dev.dtype != t.int32 or draft_dev.numel() < n * self.k_max or not draft_dev.is_contiguous()):
-            _refuse("draft_dev has to be int32 [n_req, k_max]")
+        if draft_dev is not None and (draft_dev.dtype != t.int32 or draft_dev.numel() < n * self.k_max or not draft_dev.is_contiguous()
+                                      or draft_dev.device != self._dev):
+            _refuse("draft_dev has to be int32 [n_req, k_max], on the context's device")
         if len(kk) != n:
             _refuse("k has to be one draft length for each request")
         tt, al = t.zeros((n, self.k_max + 1), dtype=t.int32, device=self._dev), t.empty(n, dtype=t.int32, device=self._dev)
@@ -544,7 +545,8 @@ def _attend_scratch(page_tokens, kv_heads, head_dim, code, heads, n_req, rows, m
 def attend_static(q, k_cache, v_cache, block_table, row_off, kv_len, *, scale: Optional[float] = None, max_len: int = 0, out=None):
     """stairs_attend_static: attention of the new rows' queries [rows, heads, head_dim] over the paged cache.  block_table: int32
     [n_req, max_blocks]; row_off: int32 [n_req + 1]; kv_len: int32 [n_req], the new rows included; scale: 1 / sqrt(head_dim) if None;
-    max_len: bound of kv_len (0: what the table can hold).  Returns `out`, by default a new tensor; rows of no request are not written."""
+    max_len: bound of kv_len (0: what the table can hold).  Returns `out`, by default a new tensor, which may not overlap q; rows of no request
+    are not written."""
     torch, lib = _t(), load_library()
     dev = _device_of(q, k_cache, v_cache, block_table, row_off, kv_len, out)
     c, kv_heads, hd = _paged(k_cache, v_cache)

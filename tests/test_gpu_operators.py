@@ -1,5 +1,7 @@
 """The operators on caller-held buffers against plain 64-bit implementations (tests/operator_util.py)."""
+import itertools
 import math
+import threading
 
 import numpy as np
 import pytest
@@ -289,6 +291,75 @@ def test_attend_strides_and_alignment(st, dtype):
             store = torch.full((12, 16, width), 3.0, dtype=d, device=DEV)
             check_attend(st, p, q, [8, 4], [50, 9], out=store[:, ::2, at:])
             assert bool((store[:, 1::2] == 3).all()) and bool((store[:, :, :at] == 3).all())
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("order", list(itertools.permutations(range(3))))
+@pytest.mark.parametrize("new", [4, 80])
+def test_attend_caches_in_any_order(st, dtype, order, new):
+    lens = [300, new]
+    p = Paged(16, DTYPES[dtype], 2, 64, 16, lens)
+    for name in ("k", "v"):                                              # pages, tokens and heads from the widest stride to the narrowest
+        c = getattr(p, name)
+        setattr(p, name, c.permute(*order, 3).contiguous().permute(*[order.index(i) for i in range(3)], 3))
+    q = torch.randn((2 * new, 4, 64), generator=p.g, device=DEV).to(DTYPES[dtype])
+    check_attend(st, p, q, [new, new], lens)
+    for name in ("k", "v"):                                              # all heads of the cache in one place
+        setattr(p, name, getattr(p, name)[:, :, :1].expand(-1, -1, 2, -1))
+    check_attend(st, p, q, [new, new], lens)
+    slots = torch.arange(3, device=DEV)                                  # and rows that all have the same keys
+    rows = torch.randn((1, 1, 64), generator=p.g, device=DEV).to(DTYPES[dtype])
+    k = torch.zeros((4, 16, 2, 64), dtype=DTYPES[dtype], device=DEV).permute(1, 0, 2, 3).contiguous().permute(1, 0, 2, 3)
+    v = torch.zeros_like(k)
+    st.append_static(rows.expand(3, 2, 64), rows.expand(3, 2, 64), k, v, slots)
+    assert torch.equal(k[0, :3], rows.expand(3, 2, 64)) and torch.equal(v, k) and not bool(k[0, 3:].any()) and not bool(k[1:].any())
+
+
+def test_calls_from_two_threads(st):
+    p = Paged(17, torch.bfloat16, 2, 64, 16, [900, 2000])
+    off, kv, rows = i32([0, 100, 200]), i32([900, 2000]), 200
+    q = torch.randn((2, rows, 8, 64), generator=p.g, device=DEV).bfloat16()
+    x, u = torch.randn((2, 6, 5000), generator=p.g, device=DEV), torch.rand(6, generator=p.g, device=DEV)
+    attend = lambda i, **kw: st.attend_static(q[i], p.k, p.v, p.table, off, kv, **kw)   # noqa: E731
+    sample = lambda i, **kw: st.sample_static(x[i], [0] * 6, None, 0, u, top_p=0.9, **kw)[0]   # noqa: E731
+    want = [(attend(i), sample(i)) for i in range(2)]
+    torch.cuda.synchronize()
+    got, errors = [[], []], []
+
+    def work(i):
+        try:
+            s = torch.cuda.Stream()
+            for _ in range(30):
+                got[i].append((attend(i, stream=s), sample(i, stream=s)))
+            s.synchronize()
+        except Exception as e:                                           # noqa: BLE001
+            errors.append(e)
+
+    threads = [threading.Thread(target=work, args=(i,)) for i in range(2)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    assert not errors
+    for i in range(2):
+        assert len(got[i]) == 30
+        for o, tokens in got[i]:
+            assert torch.equal(o, want[i][0]) and torch.equal(tokens, want[i][1])
+
+
+def test_attend_refuses_to_write_over_its_queries(st):
+    p = Paged(18, torch.bfloat16, 2, 64, 16, [30])
+    q = torch.randn((2, 4, 64), generator=p.g, device=DEV).bfloat16()
+    with pytest.raises(st.StairsError) as e:
+        st.attend_static(q, p.k, p.v, p.table, i32([0, 2]), i32([30]), out=q)
+    assert e.value.code == 1 and "over the queries" in str(e.value)
+
+
+def test_sample_numbers_outside_their_range(st):
+    x = torch.zeros((5, 100), device=DEV)
+    u = torch.tensor([1.0, 2.0, math.inf, -1.0, math.nan], device=DEV)
+    tokens, _ = st.sample_static(x, [0] * 5, None, 0, u)
+    assert tokens[:, 0].tolist() == [99, 99, 99, 0, 0]
 
 
 def test_attend_offsets_beyond_32_bits(st):

@@ -102,7 +102,8 @@ def test_sampled_calls_refuse_before_they_enqueue():
     for bad in (lambda: eng.validate_sampled([0], [7], d, u), lambda: eng.validate_sampled([1], [2], d, u), lambda: eng.validate_sampled([0, 0], [0, 0], d, u)):
         with pytest.raises((st.StairsError, ValueError)):
             bad()
-    for bad in (lambda: eng.validate_sampled([0], [2], d, u[:2]), lambda: eng.validate_sampled([0], [2], d, u.double()), lambda: eng.generate_sampled(0, [1, 2], 0, 9, u)):
+    for bad in (lambda: eng.validate_sampled([0], [2], d, u[:2]), lambda: eng.validate_sampled([0], [2], d, u.double()), lambda: eng.validate_sampled([0], [2], d.cpu(), u),
+                lambda: eng.validate_sampled([0], [2], d.long(), u), lambda: eng.generate_sampled(0, [1, 2], 0, 9, u)):
         with pytest.raises(ValueError):
             bad()
     assert eng.launch_count() == launches and eng.sequence(0) == seq

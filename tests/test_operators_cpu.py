@@ -35,10 +35,11 @@ def said(lib, rc, want, text):
     (dict(page=0), EINVAL, "page_tokens"), (dict(blocks=0), EINVAL, "max_blocks"), (dict(blocks=1 << 27, page=16), EINVAL, "31 bits"),
     (dict(n_free=-1), EINVAL, "n_free"), (dict(rows=-1), EINVAL, "max_rows"), (dict(rows=2**31 - 1), EINVAL, "max_rows"),
     (dict(blocks_out=P + 4), EINVAL, "output is its input"), (dict(used_out=P + 8), EINVAL, "output is its input"),
+    (dict(kv=P + 4), EINVAL, "output is its input"), (dict(off=P), EINVAL, "output is its input"),
     (dict(kv=P + 2), EINVAL, "aligned"), (dict(slot=P + 4), EINVAL, "aligned")])
 def test_tables_refusals(lib, bad, code, text):
     a = dict(n_req=2, n_seq=P, n_new=P, blocks_in=P + 4, table=P, blocks=8, page=16, free=P, n_free=4, used_in=P + 8, rows=10, blocks_out=P + 12,
-             used_out=P + 16, off=P, kv=P, req=P, pos=P, slot=P, served=P)
+             used_out=P + 16, off=P + 20, kv=P + 40, req=P, pos=P, slot=P, served=P)
     a.update(bad)
     said(lib, lib.stairs_tables_static(*a.values(), None), code, text)
 
@@ -56,7 +57,7 @@ def test_append_refusals(lib, bad, code, text):
 
 
 def attend(lib, **bad):
-    a = dict(c=cache(), table=P, blocks=8, n_req=2, off=P, kv=P, max_len=0, rows=3, heads=4, q=P, q_row=256, q_head=64, scale=0.125, o=P, o_row=256,
+    a = dict(c=cache(), table=P, blocks=8, n_req=2, off=P, kv=P, max_len=0, rows=3, heads=4, q=P, q_row=256, q_head=64, scale=0.125, o=P + 4096, o_row=256,
              o_head=64, ws=1 << 20, ws_bytes=1 << 40)
     a.update(bad)
     a["c"] = C.byref(a["c"]) if a["c"] is not None else None
