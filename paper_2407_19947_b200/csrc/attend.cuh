@@ -54,16 +54,19 @@ inline int am_ks(int hd) {
   for (int k : am_steps) if (hd <= 16 * k) return k;
   return 16;
 }
-// Small calls: a cluster of CTAs for every unit, as many as keep the chip's SMs (those that clusters find free) busy and have a chunk
-// each, joined through distributed shared memory: one launch, no scratch.  0: too many units or too long for that (the lengths are
-// only known by their bound, and the longest request's CTAs would work alone at the end).
+// Small calls: a cluster of CTAs for every unit, as many as keep the chip's SMs (those that clusters find free: with one CTA an SM, sixteen clusters
+// of eight do not all fit, 16 units of 40 queries, heads of 64, 23.6 us in them and 13.5 in clusters of four) busy and have a chunk each, joined through
+// distributed shared memory: one launch, no scratch.  0: too many units, or too long for that (the lengths are only known by their bound, and the longest
+// request's CTAs would work alone at the end).  Measured, cut over all CTAs against clusters, us: heads of 128, one request, 4 queries a key head of 8,
+// 512 tokens 15 and 11, 4096 22 and 20, 8192 26 and 29; 20 queries, 2048 25 and 21, 4096 27 and 27, 8192 32 and 38; 64 queries, 512 25 and 24, 2048 27
+// and 34; heads of 64, 16 key heads, 4096 18 and 16, 8192 23 and 23, 16384 28 and 36: by chunks a CTA, row groups and head size.
 inline int am_cluster(int ks, int mg, int n_rows, int n_req, int group, int kv_heads, int max_len) {
   const long long q = (long long)n_rows * group, blocks = n_req == 1 ? (q + 16 * mg - 1) / (16 * mg) : q / (16 * mg) + n_req, units = blocks * kv_heads;
-  const int chunks = (max_len + AM_CHUNK - 1) / AM_CHUNK, room = 128 * am_ctas(ks, mg);
+  const int chunks = (max_len + AM_CHUNK - 1) / AM_CHUNK, ctas = am_ctas(ks, mg), room = 128 * ctas, room_of_8 = ctas == 1 ? 112 : room;
   if (units > room) return 0;
   int s = 1;
-  while (s < 8 && units * s * 2 <= room && s < chunks) s *= 2;
-  return (chunks + s - 1) / s <= 24 ? s : 0;
+  while (s < 8 && units * s * 2 <= (s == 4 ? room_of_8 : room) && s < chunks) s *= 2;
+  return (long long)((chunks + s - 1) / s) * mg * (ks < 4 ? 4 : ks) <= 128 ? s : 0;
 }
 inline size_t am_workspace(int ks, int mg, int hd) { return (size_t)am_grid(ks, mg) * (64 + (size_t)2 * 16 * mg * (hd + 2) * 4) + 256; }
 template <int KS> int launch_mma(const AttendParams& P, int dtype, int mg, cudaStream_t st);   // KS: 16-element steps of a head

@@ -2,8 +2,9 @@
 //
 // The steps of a call lie in one list, cut into shares of equal length, so a unit's parts lie in consecutive CTAs.  A CTA files its part's
 // state (maxima, sums, weighted values) in its scratch; a second, short kernel joins the parts, in the order of the positions, so results do not depend
-// on timing.  (Measured against joins by the CTA that is the last to file a part: four requests of 16384, one token each, 64 us against 79; one request, heads of 64, 32
-// against 43.  Where units are of 256 queries and have two or three parts, the last one joins from its registers: a chunk of 2048 rows 233 us with the kernel, 224 without.)
+// on timing.  (Against joins by the CTA that is the last to file a part, when both were built: four requests of 16384, one token each, 64 us and 79; one
+// request, heads of 64, 32 and 43.  Where units are of 256 queries and have two or three parts, the last one joins from its registers: a chunk of 2048
+// rows after 4096 took 233 us with the kernel and 224 without.)
 #pragma once
 #include <type_traits>
 
@@ -30,6 +31,12 @@ __device__ __forceinline__ int share_of(long long total, long long ctas, long lo
   while (b > 0 && share_begin(total, ctas, b) > x) --b;
   while (b + 1 < ctas && share_begin(total, ctas, b + 1) <= x) ++b;
   return (int)b;
+}
+
+// CTAs that have a share: all of them, but at least `least` steps each, so that there are fewer parts to join, or a unit each where units are shorter than that.
+__device__ __forceinline__ long long share_count(const AttendParams& P, int rows, long long total, int least) {
+  const long long q = (long long)P.n_rows * (P.heads / P.kv_heads), units = max((q + rows - 1) / rows, (long long)P.n_req) * P.kv_heads;   // (about)
+  return min(min((long long)gridDim.x, total), max((total + least - 1) / least, units));
 }
 
 // A cut unit of steps [u0, u1): its parts lie in CTAs owner .. owner + parts - 1.  Every CTA has two places for states: one for the part that its share
@@ -109,7 +116,12 @@ template <typename T, int ROWS, bool COLS> __global__ void __launch_bounds__(128
 
 template <typename T, int ROWS, bool COLS> int launch_join(const AttendParams& P, int ctas, cudaStream_t st) {
   cudaLaunchConfig_t cfg{};
-  cfg.gridDim = dim3(ctas, 4); cfg.blockDim = dim3(128); cfg.stream = st;
+  // blocks for a cut unit: more where there are few units to cut (one request of 16384 tokens, 8 key heads of 128: 36 queries each 49 us with four blocks,
+  // 42 with sixteen; 132 queries 75 and 57)
+  const long long units = ((long long)P.n_rows * (P.heads / P.kv_heads) / ROWS + P.n_req) * P.kv_heads;
+  int each = 4;
+  while (each < 16 && each * 2 * units <= 4 * AM_SMS) each *= 2;
+  cfg.gridDim = dim3(ctas, each); cfg.blockDim = dim3(128); cfg.stream = st;
   cudaLaunchAttribute at[1];
   at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization; at[0].val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = at; cfg.numAttrs = 1;

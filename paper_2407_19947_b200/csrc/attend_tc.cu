@@ -13,6 +13,8 @@
 // outside the tensor and arrive as zeros), 9 MMA issue and TMEM, 10-11 queries (16-byte asynchronous copies: any strides) and the values of chunks that
 // reach past some query's last position: what lies behind the request's end is cleared, and infinities and NaN are taken out, since
 // 0 * infinity in a product would carry them to rows that do not see them; rows that do get them added at the end.
+// Measured, 8 key heads of 128 with four query heads each: 2048 rows after 4096, 172 GFLOP: 217 us, 0.79 PFLOP/s; four requests of 16384, 9 rows each (narrow), 269 MB:
+// 82 us, 3.3 TB/s; 512 rows of a new request 52 us, of which a unit's way from its queries to its results is nearly all.
 // The steps (request, 256 queries, key head, 128 positions; only visible ones) form one list, cut evenly over the CTAs; units cut over
 // CTAs are joined by a second kernel, or, wide, 32 queries at a time by the warp that is the last to have its part (see attend_parts.cuh).
 #include <cuda.h>
@@ -103,6 +105,7 @@ struct Unit { int req, first, n, len, qb, h, nch[2], all, c; };   // all: chunks
 // queries, both tiles on them, chunks of 64 positions in more stages: K and V are what it waits for.
 template <bool NARROW> struct Form {
   static constexpr int CH = NARROW ? 64 : 128, ROWS = NARROW ? 128 : 256, NST = NARROW ? 5 : 2, Q_TILES = NARROW ? 1 : 2;
+  static constexpr int LEAST = NARROW ? 4 : 1;     // chunks that a CTA has at least (see share_count; wide, 3 measured the same)
   static __device__ __forceinline__ int tile_chunks(int n, int len, int q0, int group) {
     const int nq = min(n * group - q0, 128);
     if (nq <= 0) return 0;
@@ -215,7 +218,7 @@ __global__ void __launch_bounds__(AT_THREADS, 1) k_attend_tc(const __grid_consta
   };
   long long total = 0, x0 = 0, x1 = 0, ctas;
   auto shares = [&]() {
-    ctas = min((long long)gridDim.x, total);
+    ctas = share_count(P, AT_ROWS, total, F::LEAST);
     if (blockIdx.x < ctas) { x0 = share_begin(total, ctas, blockIdx.x); x1 = share_begin(total, ctas, blockIdx.x + 1); }
   };
   auto start = [&](int req, const Span& sp, int qb, long long rem) {   // rem: steps of block qb before this CTA's first one
@@ -439,22 +442,30 @@ __global__ void __launch_bounds__(AT_THREADS, 1) k_attend_tc(const __grid_consta
     __syncwarp();
   } else if (warp >= 10) {
     // ------------------------------------------------------------------ queries, and values of chunks at the edge
-    const int ft = tid - 320, pieces = P.hd / 8;
+    constexpr int PC = HD / 8, STEP = 64 / PC;       // rows that the 64 threads take at a time
+    const int ft = tid - 320, pieces = P.hd / 8, col = ft % PC, row0 = ft / PC;
     int it = 0, edges[NST] = {};
     bool ok = true;
     while (ok && W.begin(c0, c1)) {
       const Unit& u = W.u;
       ok = __all_sync(0xffffffffu, mbar_wait(q_empty, (W.seg & 1) ^ 1, abort_flag, AT_WAIT));
       if (!ok) break;
-      constexpr int PC = HD / 8;
       const Sh sh(u, c0, c1);
-#pragma unroll 4
-      for (int i = ft; i < AT_ROWS * PC; i += 64) {
-        const int r = i / PC, c = i % PC, qi = u.qb * AT_ROWS + r, j = qi / group;
-        const bool on = j < u.n && c < pieces;
-        const T* src = reinterpret_cast<const T*>(P.q) + (on ? (u.first + j) * P.q_row + (u.h * group + qi - j * group) * P.q_head + c * 8 : 0);
-        const uint32_t dst = smem_u32(qs) + (r >> 7) * QTILE + (c >> 3) * (128 * 128) + (r & 127) * 128 + (((c & 7) ^ (r & 7)) << 4);
-        asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(on ? 16 : 0));
+      {
+        // (a thread keeps its 16-byte column and steps through the rows: no division, every one of the two warps' instructions is time before a unit's first product)
+        int j = (u.qb * AT_ROWS + row0) / group, hg = u.qb * AT_ROWS + row0 - j * group;
+        const int dj = STEP / group, dh = STEP - dj * group, n = u.n;
+        const T* qb = reinterpret_cast<const T*>(P.q) + u.first * P.q_row + (long long)u.h * group * P.q_head + col * 8;
+        const uint32_t dst = smem_u32(qs) + (col >> 3) * (128 * 128);
+#pragma unroll 8
+        for (int i = 0; i < AT_ROWS / STEP; ++i) {
+          const int r = row0 + i * STEP;
+          const bool on = j < n && col < pieces;
+          const T* src = on ? qb + j * P.q_row + hg * P.q_head : reinterpret_cast<const T*>(P.q);
+          asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst + (r >> 7) * QTILE + (r & 127) * 128 + (((col & 7) ^ (r & 7)) << 4)), "l"(src), "r"(on ? 16 : 0));
+          j += dj; hg += dh;
+          if (hg >= group) { hg -= group; ++j; }
+        }
       }
       asm volatile("cp.async.commit_group;\n\tcp.async.wait_group 0;" ::: "memory");
       asm volatile("fence.proxy.async.shared::cta;" ::: "memory");   // the tensor core reads these tiles through the async proxy
@@ -469,23 +480,33 @@ __global__ void __launch_bounds__(AT_THREADS, 1) k_attend_tc(const __grid_consta
         ok = __all_sync(0xffffffffu, mbar_wait(e_full + s, edges[s] & 1, abort_flag, AT_WAIT));
         ++edges[s];
         if (!ok) break;
-        constexpr uint32_t EXPO = BF ? 0x7f80u : 0x7c00u;
+        constexpr uint32_t EXPO = BF ? 0x7f807f80u : 0x7c007c00u, ONE = BF ? 0x00800080u : 0x04000400u;
         const int left = u.len - (c0 + j) * AT_CH;   // positions of the chunk that the request has
+        uint8_t* column = vst + (size_t)s * KBYTES + (col >> 3) * (AT_CH * 128);
+        auto place = [&](int r) { return reinterpret_cast<uint4*>(column + r * 128 + (((col & 7) ^ (r & 7)) << 4)); };
         bool odd = false;
-        for (int i = ft; i < AT_CH * PC; i += 64) {
-          const int r = i / PC, c = i % PC;
-          uint4* at = reinterpret_cast<uint4*>(vst + (size_t)s * KBYTES + (c >> 3) * (AT_CH * 128) + r * 128 + (((c & 7) ^ (r & 7)) << 4));
-          if (r >= left) { *at = make_uint4(0u, 0u, 0u, 0u); continue; }
-          uint4 w = *at;
-          uint32_t* e = reinterpret_cast<uint32_t*>(&w);
-          bool hit = false;
+#pragma unroll 1
+        for (int r0 = row0; r0 < AT_CH; r0 += 4 * STEP) {   // four pieces' loads under way together
+          uint4 w[4];
 #pragma unroll
-          for (int x = 0; x < 4; ++x) {
-            const uint32_t keep = ((e[x] & EXPO) == EXPO ? 0u : 0xffffu) | (((e[x] >> 16) & EXPO) == EXPO ? 0u : 0xffff0000u);
-            hit = hit || keep != 0xffffffffu;
-            e[x] &= keep;
+          for (int k = 0; k < 4; ++k) w[k] = *place(r0 + k * STEP);
+#pragma unroll
+          for (int k = 0; k < 4; ++k) {
+            const int r = r0 + k * STEP;
+            uint32_t* e = reinterpret_cast<uint32_t*>(&w[k]);
+            // an exponent of ones and one more: a carry into the sign's place
+            const uint32_t hit = (((e[0] & EXPO) + ONE) | ((e[1] & EXPO) + ONE) | ((e[2] & EXPO) + ONE) | ((e[3] & EXPO) + ONE)) & 0x80008000u;
+            if (r >= left) *place(r) = make_uint4(0u, 0u, 0u, 0u);
+            else if (hit) {
+#pragma unroll
+              for (int x = 0; x < 4; ++x) {
+                const uint32_t c = ((e[x] & EXPO) + ONE) & 0x80008000u;
+                e[x] &= ~((c >> 15) * 0xffffu);      // (a half that carries becomes zero)
+              }
+              *place(r) = w[k];
+              odd = true;
+            }
           }
-          if (hit) { *at = w; odd = true; }
         }
         if (odd) *odd_flag = 1;
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
@@ -668,6 +689,14 @@ __global__ void __launch_bounds__(AT_THREADS, 1) k_attend_tc(const __grid_consta
           }
         }
       };
+      T* rows_of_lane[2] = {nullptr, nullptr};         // where this lane stores of the warp's rows lane / 2 and 16 + lane / 2
+      if (put) {
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+          const int q2 = qi - lane + k * 16 + (lane >> 1), j2 = q2 / group;
+          if (j2 < u.n) rows_of_lane[k] = reinterpret_cast<T*>(P.o) + (u.first + j2) * P.o_row + (u.h * group + q2 - j2 * group) * P.o_head + (lane & 1) * 8;
+        }
+      }
       auto store = [&](uint32_t* v, int d) {           // a row a thread -> two lanes a row: stores of whole 32-byte sectors
 #pragma unroll
         for (int g = 0; g < 2; ++g) {
@@ -678,15 +707,14 @@ __global__ void __launch_bounds__(AT_THREADS, 1) k_attend_tc(const __grid_consta
           __syncwarp();
 #pragma unroll
           for (int k = 0; k < 2; ++k) {
-            const int r = k * 16 + (lane >> 1), c = (lane & 1) * 8, dc = d + g * 16 + c, q2 = qi - lane + r;
-            if (q2 < u.n * group && dc < P.hd) {
+            const int r = k * 16 + (lane >> 1), c = (lane & 1) * 8;
+            if (rows_of_lane[k] && d + g * 16 + c < P.hd) {
               const float* s = tile + r * 20 + c;
               const float k2 = tile[r * 20 + 16];
               uint4 w;
               w.x = pack2<T>(s[0] * k2, s[1] * k2); w.y = pack2<T>(s[2] * k2, s[3] * k2);
               w.z = pack2<T>(s[4] * k2, s[5] * k2); w.w = pack2<T>(s[6] * k2, s[7] * k2);
-              const int j2 = q2 / group;
-              *reinterpret_cast<uint4*>(reinterpret_cast<T*>(P.o) + (u.first + j2) * P.o_row + (u.h * group + q2 - j2 * group) * P.o_head + dc) = w;
+              *reinterpret_cast<uint4*>(rows_of_lane[k] + d + g * 16) = w;
             }
           }
         }
